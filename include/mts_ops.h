@@ -1,0 +1,212 @@
+/*
+ * mts_ops.h -- what one serving instance computes in a tick, on MI355X (gfx950).
+ *
+ * mts.h schedules serving instances and counts their KV blocks; the operators
+ * here run on such a pool of blocks.  A request's tokens are its slots
+ * 0 .. len-1; slot j lies in block table[j / block_tokens] at offset
+ * j % block_tokens.  One tick of one layer:
+ *   mts_rope    rotary positions of the new tokens' queries and keys; keys,
+ *               values and positions go to the new tokens' slots
+ *   mts_attend  attention of the new tokens (one per request, a tree of
+ *               drafted ones, or a chunk of a prompt) over the request's slots
+ *   mts_weigh   the attention weight every slot has received, accumulated
+ *   mts_evict   requests over their budget of slots keep the most attended
+ *   mts_sample  the next token from the logits and a given random number
+ *
+ * Conventions: as in mts.h.  Every function returns MTS_OK or a negative
+ * MTS_E* code and never throws.  Unless a field says otherwise its pointer is
+ * device memory owned by the caller, all work is enqueued on the given stream
+ * and the call returns after the launches; nothing is allocated and the calls
+ * can be captured into a graph.  Arrays on the device cannot be checked by the
+ * host: kernels clamp lengths to the table and token ranges to the arrays
+ * (q_start must not fall), and a block id outside the pool makes its slots
+ * unattended, unweighed, unwritten.  Strides are in elements.  Tensors of 16-bit types need 16-byte
+ * aligned pointers and strides that are multiples of 8 (mts_sample: none).
+ */
+#ifndef MTS_OPS_H
+#define MTS_OPS_H
+
+#include "mts.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* element types */
+enum { MTS_BF16 = 0, MTS_F16 = 1, MTS_F32 = 2 };
+/* rotary pairs: (i, i + rot/2), or (2i, 2i + 1) */
+enum { MTS_ROPE_HALF = 0, MTS_ROPE_INTERLEAVED = 1 };
+/* frequency scaling for contexts longer than the trained one */
+enum { MTS_ROPE_PLAIN = 0,    /* f_i = base^(-2i/rot) */
+       MTS_ROPE_LINEAR = 1,   /* f_i / factor */
+       MTS_ROPE_BASE = 2,     /* base * factor^(rot / (rot - 2)): the slowest pair is divided by factor, the fastest kept */
+       MTS_ROPE_PARTS = 3 };  /* pairs that turn at least `fast` times over the trained context are kept, those that turn at
+                                 most `slow` times are divided by factor, a ramp between */
+
+/* One layer's pool of KV blocks. */
+typedef struct mts_pool {
+    void* k;                      /* NULL where an operator does not take it */
+    void* v;
+    int64_t k_block, k_head, k_token; /* strides; a token's head_dim elements are contiguous */
+    int64_t v_block, v_head, v_token;
+    uint32_t n_blocks;            /* blocks in the pool, 1 .. 2^31 - 1 */
+    uint32_t block_tokens;        /* power of two, 1..64 */
+    uint32_t kv_heads;            /* 1 .. 65535 */
+    uint32_t head_dim;            /* 64, 96, 128 or 256 (mts_rope: any multiple of 8 up to 512) */
+    uint32_t type;                /* MTS_BF16, MTS_F16 (mts_rope without a pool also MTS_F32) */
+    uint32_t reserved;            /* must be 0 */
+} mts_pool;
+
+/* The requests of a call and where their slots lie. */
+typedef struct mts_batch {
+    const int32_t* table;         /* [n][table_width] block ids; entries past a request's length are not read */
+    const int32_t* lens;          /* [n] slots of each request, the new tokens' among them */
+    const int32_t* q_start;       /* [n + 1] first new token of each request among the n_tokens; not read by mts_evict */
+    const uint64_t* tree;         /* [n_tokens][tree_words]: bit i of a token: it attends its request's i-th new token;
+                                     NULL: new tokens attend those before them and themselves */
+    uint32_t n;                   /* requests; 0: nothing is done */
+    uint32_t table_width;         /* >= 1; table_width * block_tokens <= 2^30 */
+    uint32_t n_tokens;            /* new tokens of all requests */
+    uint32_t max_q;               /* at least the new tokens of any request (tokens past it are not computed) */
+    uint32_t tree_words;          /* 0 if tree is NULL */
+    uint32_t reserved;            /* must be 0 */
+} mts_batch;
+
+/* Rotary positions.  freqs[i] is the angle in radians that a position turns
+ * pair i by; the angle is formed in 64 bits, its sine and cosine in 32:
+ *   (x, y) -> mscale (x cos - y sin, x sin + y cos),  inverse: sin -> -sin.
+ * The inverse is the gradient's rotation (and undoes the forward one when
+ * mscale is 1).  Elements rot .. head_dim-1 are copied.  q and k may be NULL
+ * (with 0 heads), q_out == q and k_out == k rotate in place.  With slots, k's
+ * rows go to pool.k (and v's to pool.v where v is not NULL) at slot
+ * slots[token] = block * block_tokens + offset instead of k_out, and the token's position to pos
+ * ([n_blocks][kv_heads][block_tokens], may be NULL); a slot outside the pool
+ * (such as -1) writes nothing.  Two tokens of a call must not share a slot. */
+typedef struct mts_rope_args {
+    const void *q, *k, *v;        /* [n_tokens][heads][head_dim] by strides */
+    void *q_out, *k_out;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head;
+    int64_t qo_token, qo_head, ko_token, ko_head;
+    const int32_t* positions;     /* [n_tokens] */
+    const double* freqs;          /* [rot / 2] */
+    const int64_t* slots;         /* [n_tokens] or NULL */
+    int32_t* pos;
+    mts_pool pool;                /* type, kv_heads and head_dim hold for q and k also without slots */
+    uint32_t n_tokens, q_heads;
+    uint32_t rot;                 /* even, 2 .. head_dim */
+    uint32_t layout;              /* MTS_ROPE_HALF, MTS_ROPE_INTERLEAVED */
+    uint32_t inverse;             /* 0 or 1 */
+    float mscale;
+} mts_rope_args;
+int mts_rope(const mts_rope_args* args, hipStream_t stream);
+
+/* Fill freqs[rot / 2] (host memory) for the formulas above.  `trained` is the
+ * context the model was trained on, `fast` and `slow` turns bound PARTS' ramp. */
+int mts_rope_freqs(double* freqs, uint32_t rot, double base, uint32_t scaling, double factor, double trained,
+                   double fast, double slow);
+
+/* Attention over the pool.  Query head h attends KV head h / (q_heads /
+ * kv_heads).  out = sum_j p_j v_j with p the softmax of scale * q.k over the
+ * slots that the token may see: all before the request's new tokens, and of
+ * these what tree or their order allows.  lse (may be NULL) gets the logarithm
+ * of the softmax's sum.  A token that sees nothing gets zeros and -inf.  What
+ * an unseen slot holds (also NaN) has no effect.  Scores, sums and the
+ * accumulated output are held in 32 bits; the weights are rounded to the
+ * pool's type for the product with the values. */
+typedef struct mts_attend_args {
+    mts_pool pool;
+    mts_batch batch;
+    const void* q;                /* [n_tokens][q_heads][head_dim] by strides, the pool's type */
+    void* out;                    /* the same shape */
+    float* lse;                   /* [n_tokens][q_heads] or NULL */
+    int64_t q_token, q_head, out_token, out_head;
+    uint32_t q_heads;             /* a multiple of kv_heads */
+    float scale;
+    void* workspace;              /* at least mts_attend_workspace bytes, 256-byte aligned.  Zero before its first use; calls
+                                     leave it so that the next one in stream order can use it, whatever its sizes */
+    size_t workspace_bytes;       /* the same for every call with this workspace */
+} mts_attend_args;
+int mts_attend(const mts_attend_args* args, hipStream_t stream);
+/* Bytes for calls of at most these sizes. */
+int mts_attend_workspace(uint32_t n, uint32_t n_tokens, uint32_t max_q, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
+                         size_t* bytes);
+
+/* Accumulated attention weights: for every slot and KV head
+ *   score = decay * score + sum over the new tokens that see it and the
+ *           group's query heads of exp(scale * q.k - lse)
+ * The slots of the call's own new tokens start from zero, and with decay 0
+ * every slot does (what the array held there is not read).  Rows with lse
+ * -inf add nothing; requests without new tokens are left as they are. */
+typedef struct mts_weigh_args {
+    mts_pool pool;                /* k only */
+    mts_batch batch;
+    const void* q;
+    const float* lse;             /* [n_tokens][q_heads], as mts_attend gave it */
+    int64_t q_token, q_head;
+    float* score;                 /* [n_blocks][kv_heads][block_tokens] */
+    uint32_t q_heads;
+    float scale, decay;
+} mts_weigh_args;
+int mts_weigh(const mts_weigh_args* args, hipStream_t stream);
+
+/* Eviction.  A request with more than `budget` slots keeps, in every KV head
+ * for itself, `budget` of them: first those whose position is below `sink` or
+ * at least next_pos - recent, then those of the largest score (NaN counts as
+ * -inf), equal ones by the lowest slot.  Kept slots below the budget stay, the
+ * i-th kept one at or above it moves to the i-th given up below it, keys,
+ * values, score and position together: the order of slots is not the order of
+ * positions afterwards, which the attention of rotated keys does not ask for.
+ * lens_out[r] = min(len, budget); the blocks past it are free again.
+ * score_out and pos_out may be the inputs; otherwise their slots 0 ..
+ * lens_out-1 are written.  A moved slot whose block is outside the pool is
+ * not copied. */
+typedef struct mts_evict_args {
+    mts_pool pool;
+    mts_batch batch;
+    const float* score;           /* [n_blocks][kv_heads][block_tokens] */
+    const int32_t* pos;           /* the same shape */
+    const int32_t* next_pos;      /* [n] position of the request's next token */
+    float* score_out;
+    int32_t* pos_out;
+    int32_t* lens_out;            /* [n], not lens */
+    uint32_t budget;              /* >= 1 */
+    uint32_t recent, sink;
+    uint32_t reserved;            /* must be 0 */
+    void* workspace;              /* mts_evict_workspace bytes, 256-byte aligned, of any contents */
+    size_t workspace_bytes;
+} mts_evict_args;
+int mts_evict(const mts_evict_args* args, hipStream_t stream);
+int mts_evict_workspace(uint32_t n, uint32_t kv_heads, uint32_t table_width, uint32_t block_tokens, uint32_t budget, size_t* bytes);
+
+/* The next token of every row of logits.  With w_i = exp((l_i - max) /
+ * temperature), rounded to 32 bits, and tokens ranked by logit, equal ones by
+ * the lowest index:
+ *   top_k  > 0: the first top_k ranks are kept
+ *   top_p  < 1: of these, rank after rank while the sum of the ones before is
+ *               below top_p times the sum of all that top_k kept
+ *   min_p  > 0: of these, the ones with w_i >= min_p (above 1 it counts as 1)
+ * and the token is the first in vocabulary order whose cumulative kept weight
+ * exceeds u times the kept sum; sums are carried in 64 bits.  logprob is the
+ * logarithm of its share of the kept sum.  temperature <= 0: the first rank,
+ * logprob 0.  NaN counts as -inf; a row without any larger logit gives -1 and
+ * -inf.  Logits of +inf share the whole weight. */
+typedef struct mts_sample_args {
+    const void* logits;           /* [rows][vocab], row_stride apart */
+    int64_t row_stride;
+    const float* u;               /* [rows] in [0, 1) */
+    const float* temperature;     /* [rows] */
+    const int32_t* top_k;         /* [rows]; <= 0: off */
+    const float* top_p;           /* [rows]; >= 1: off; <= 0: the first rank */
+    const float* min_p;           /* [rows]; <= 0: off */
+    int32_t* token;               /* [rows] */
+    float* logprob;               /* [rows] or NULL */
+    uint32_t rows, vocab;         /* vocab 1 .. 2^24 */
+    uint32_t type;                /* MTS_BF16, MTS_F16, MTS_F32 */
+    uint32_t reserved;            /* must be 0 */
+} mts_sample_args;
+int mts_sample(const mts_sample_args* args, hipStream_t stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* MTS_OPS_H */

@@ -1,0 +1,80 @@
+// Declarations shared by the operators' translation units: host-side checks
+// and the device-side view of a pool and a batch.
+#pragma once
+
+#include <cstddef>
+#include <cstdint>
+
+#include <hip/hip_runtime.h>
+
+#include "mts_ops.h"
+
+namespace mts {
+namespace ops {
+
+constexpr uint32_t kMaxHeads = 65535;
+// largest power of two that slot indices of one request stay at or below
+constexpr uint64_t kMaxSlots = 1ull << 30;
+
+inline bool aligned(const void* p, size_t a) { return p && reinterpret_cast<uintptr_t>(p) % a == 0; }
+inline bool stride8(int64_t s) { return s % 8 == 0 && s >= 0; }
+inline uint32_t log2u(uint32_t v) { return uint32_t(__builtin_ctz(v)); }
+inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
+inline size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
+
+inline bool head_dim_ok(uint32_t d) { return d == 64 || d == 96 || d == 128 || d == 256; }
+
+// What every operator on a pool asks of it.  need_k / need_v: that tensor is read or written.
+inline bool pool_ok(const mts_pool& p, bool need_k, bool need_v)
+{
+    if (p.reserved || p.n_blocks < 1 || p.n_blocks > 0x7fffffffu) return false;
+    if (p.block_tokens < 1 || p.block_tokens > 64 || (p.block_tokens & (p.block_tokens - 1))) return false;
+    if (p.kv_heads < 1 || p.kv_heads > kMaxHeads || (p.type != MTS_BF16 && p.type != MTS_F16)) return false;
+    if (need_k && !(aligned(p.k, 16) && stride8(p.k_block) && stride8(p.k_head) && stride8(p.k_token))) return false;
+    if (need_v && !(aligned(p.v, 16) && stride8(p.v_block) && stride8(p.v_head) && stride8(p.v_token))) return false;
+    return true;
+}
+
+inline bool batch_ok(const mts_batch& b, uint32_t block_tokens, bool queries)
+{
+    if (b.reserved || b.n > 0x7ffffffu || b.tree_words > 1024) return false;
+    if (b.n == 0) return true;  // a call without requests does nothing
+    if (!b.table || !b.lens || b.table_width < 1) return false;
+    if (uint64_t(b.table_width) * block_tokens > kMaxSlots) return false;
+    if (!queries) return true;
+    if (!b.q_start || b.n_tokens > 0x7fffffffu || b.max_q < 1 || b.max_q > 0x7fffffffu) return false;
+    return b.tree ? b.tree_words >= 1 : b.tree_words == 0;
+}
+
+// Device view: what the kernels take by value.
+struct Pool {
+    const char* k;
+    const char* v;
+    int64_t k_block, k_head, k_token, v_block, v_head, v_token;  // bytes
+    uint32_t n_blocks, lb, kv_heads;                             // lb: log2 of block_tokens
+};
+
+struct Batch {
+    const int32_t* table;
+    const int32_t* lens;
+    const int32_t* q_start;
+    const uint64_t* tree;
+    int32_t n, width, n_tokens, max_q, words;
+};
+
+inline Pool device_pool(const mts_pool& p)
+{
+    return Pool{static_cast<const char*>(p.k), static_cast<const char*>(p.v), 2 * p.k_block, 2 * p.k_head, 2 * p.k_token,
+                2 * p.v_block, 2 * p.v_head, 2 * p.v_token, p.n_blocks, log2u(p.block_tokens), p.kv_heads};
+}
+
+inline Batch device_batch(const mts_batch& b)
+{
+    return Batch{b.table, b.lens, b.q_start, b.tree, int32_t(b.n), int32_t(b.table_width), int32_t(b.n_tokens),
+                 int32_t(b.max_q), int32_t(b.tree_words)};
+}
+
+inline int launched() { return hipGetLastError() == hipSuccess ? MTS_OK : MTS_EDEVICE; }
+
+}  // namespace ops
+}  // namespace mts

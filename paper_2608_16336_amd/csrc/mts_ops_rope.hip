@@ -1,0 +1,202 @@
+// Rotary positions and the append to the paged cache (mts_rope).
+#include <cmath>
+
+#include "mts_ops_dev.h"
+
+namespace mts {
+namespace ops {
+
+struct RopeP {
+    const char *q, *k, *v;
+    char *qo, *ko;
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, qo_token, qo_head, ko_token, ko_head;  // bytes
+    const int32_t* positions;
+    const double* freqs;
+    const int64_t* slots;
+    int32_t* pos;
+    char *kc, *vc;
+    int64_t kc_block, kc_head, kc_token, vc_block, vc_head, vc_token;  // bytes
+    int64_t n_slots;
+    int lb, q_heads, kv_heads, D, rot, n_tokens;
+    float mscale, sign;
+};
+
+template <class E, int V>
+struct alignas(sizeof(E) * V) Vec {
+    E x[V];
+};
+
+// One workgroup a token.  The angles' sines and cosines are formed once, in
+// LDS; then every thread turns pieces of 2 V elements (V pairs) of any head:
+// V from each half of the rotated part, or V pairs side by side.
+//
+// pos * freq has more digits than 32 bits hold from a few thousand positions
+// on: the number of whole turns is taken off in 64 bits, what is left (at
+// most half a turn) goes to 32.
+template <class E, int V, bool INTER>
+__global__ __launch_bounds__(256) void k_rope(const RopeP p)
+{
+    extern __shared__ float cs[];  // cos, then sin, of rot / 2 pairs
+    const int tok = blockIdx.x, half = p.rot / 2;
+    const int position = p.positions[tok];
+    for (int i = threadIdx.x; i < half; i += blockDim.x) {
+        const double turns = double(position) * p.freqs[i] * 0.15915494309189533577;  // 1 / 2 pi
+        float s, c;
+        sincospif(2.f * float(turns - rint(turns)), &s, &c);
+        cs[i] = c * p.mscale;
+        cs[half + i] = s * p.mscale * p.sign;
+    }
+    const int64_t slot = p.slots ? p.slots[tok] : 0;
+    const bool store = slot >= 0 && slot < p.n_slots;  // whether k and v have a place
+    const int64_t block = slot >> p.lb, off = slot & ((1 << p.lb) - 1);
+    __syncthreads();
+    const int turn = half / V, rest = (p.D - p.rot) / V, per = turn + rest, all = p.D / V;
+    const int units = (p.q_heads + p.kv_heads) * per + (p.v ? p.kv_heads * all : 0);
+    for (int u = threadIdx.x; u < units; u += blockDim.x) {
+        const int rotated = (p.q_heads + p.kv_heads) * per;
+        if (u >= rotated) {
+            const int h = (u - rotated) / all, d = (u - rotated) % all * V;
+            if (!store) continue;
+            *reinterpret_cast<Vec<E, V>*>(p.vc + block * p.vc_block + h * p.vc_head + off * p.vc_token + d * sizeof(E)) =
+                *reinterpret_cast<const Vec<E, V>*>(p.v + tok * p.v_token + h * p.v_head + d * sizeof(E));
+            continue;
+        }
+        int h = u / per;
+        const int i = u % per;
+        const char* src;
+        char* dst;
+        if (h < p.q_heads) {
+            src = p.q + tok * p.q_token + h * p.q_head;
+            dst = p.qo + tok * p.qo_token + h * p.qo_head;
+        } else {
+            h -= p.q_heads;
+            if (!store) continue;
+            src = p.k + tok * p.k_token + h * p.k_head;
+            dst = p.slots ? p.kc + block * p.kc_block + h * p.kc_head + off * p.kc_token : p.ko + tok * p.ko_token + h * p.ko_head;
+        }
+        if (i >= turn) {
+            const size_t d = (p.rot + (i - turn) * V) * sizeof(E);
+            *reinterpret_cast<Vec<E, V>*>(dst + d) = *reinterpret_cast<const Vec<E, V>*>(src + d);
+            continue;
+        }
+        const int f = i * V;  // first pair
+        const size_t d0 = (INTER ? 2 * f : f) * sizeof(E), d1 = (INTER ? 2 * f + V : half + f) * sizeof(E);
+        const Vec<E, V> a = *reinterpret_cast<const Vec<E, V>*>(src + d0), b = *reinterpret_cast<const Vec<E, V>*>(src + d1);
+        Vec<E, V> ra, rb;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            const float c = cs[f + e], s = cs[half + f + e];
+            const int lo = INTER ? 2 * e : e, hi = INTER ? 2 * e + 1 : V + e;
+            const float x = float(lo < V ? a.x[lo] : b.x[lo - V]), y = float(hi < V ? a.x[hi] : b.x[hi - V]);
+            const E rx = E(x * c - y * s), ry = E(x * s + y * c);
+            (lo < V ? ra.x[lo] : rb.x[lo - V]) = rx;
+            (hi < V ? ra.x[hi] : rb.x[hi - V]) = ry;
+        }
+        *reinterpret_cast<Vec<E, V>*>(dst + d0) = ra;
+        *reinterpret_cast<Vec<E, V>*>(dst + d1) = rb;
+    }
+    if (p.slots && p.pos && store)
+        for (int h = threadIdx.x; h < p.kv_heads; h += blockDim.x) p.pos[((block * p.kv_heads + h) << p.lb) + off] = position;
+}
+
+template <class E, int V>
+static void launch_rope(const RopeP& p, bool inter, hipStream_t stream)
+{
+    const size_t lds = sizeof(float) * p.rot;
+    if (inter)
+        hipLaunchKernelGGL((k_rope<E, V, true>), dim3(p.n_tokens), dim3(256), lds, stream, p);
+    else
+        hipLaunchKernelGGL((k_rope<E, V, false>), dim3(p.n_tokens), dim3(256), lds, stream, p);
+}
+
+}  // namespace ops
+}  // namespace mts
+
+using namespace mts::ops;
+
+extern "C" {
+
+int mts_rope_freqs(double* freqs, uint32_t rot, double base, uint32_t scaling, double factor, double trained, double fast, double slow)
+{
+    if (!freqs || rot < 2 || rot % 2 || rot > 512 || !(base > 0.0) || !std::isfinite(base) || scaling > MTS_ROPE_PARTS)
+        return MTS_EINVAL;
+    if (scaling != MTS_ROPE_PLAIN && !(factor >= 1.0 && std::isfinite(factor))) return MTS_EINVAL;
+    if (scaling == MTS_ROPE_BASE && rot < 4) return MTS_EINVAL;
+    if (scaling == MTS_ROPE_PARTS && !(trained > 0.0 && std::isfinite(trained) && slow > 0.0 && fast > slow && std::isfinite(fast)))
+        return MTS_EINVAL;
+    if (scaling == MTS_ROPE_BASE) base *= std::pow(factor, double(rot) / (rot - 2));
+    for (uint32_t i = 0; i < rot / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rot);
+        if (scaling == MTS_ROPE_LINEAR) f /= factor;
+        if (scaling == MTS_ROPE_PARTS) {
+            const double turns = trained * f / 6.283185307179586477;
+            double keep = (turns - slow) / (fast - slow);
+            keep = keep < 0.0 ? 0.0 : keep > 1.0 ? 1.0 : keep;
+            f = f * keep + f / factor * (1.0 - keep);
+        }
+        freqs[i] = f;
+    }
+    return MTS_OK;
+}
+
+int mts_rope(const mts_rope_args* a, hipStream_t stream)
+{
+    if (!a) return MTS_EINVAL;
+    const mts_pool& c = a->pool;
+    const bool cached = a->slots != nullptr;
+    const uint32_t D = c.head_dim;
+    if (c.type > MTS_F32 || D < 8 || D > 512 || D % 8 || a->rot < 2 || a->rot % 2 || a->rot > D || c.reserved) return MTS_EINVAL;
+    if (a->layout > MTS_ROPE_INTERLEAVED || a->inverse > 1 || !(a->mscale == a->mscale)) return MTS_EINVAL;
+    if (a->q_heads > kMaxHeads || c.kv_heads > kMaxHeads || a->q_heads + c.kv_heads == 0) return MTS_EINVAL;
+    if (a->n_tokens > 0x7fffffffu) return MTS_EINVAL;
+    if (cached && (!pool_ok(c, c.kv_heads != 0, a->v != nullptr) || c.kv_heads == 0)) return MTS_EINVAL;
+    if (!cached && (a->v || a->pos)) return MTS_EINVAL;
+    if (a->n_tokens == 0) return MTS_OK;
+    if (!a->positions || !a->freqs) return MTS_EINVAL;
+    const int64_t unit = c.type == MTS_F32 ? 4 : 8;
+    const auto ok = [&](const void* x, int64_t t, int64_t h) { return aligned(x, 16) && t >= 0 && h >= 0 && t % unit == 0 && h % unit == 0; };
+    if (a->q_heads && !(ok(a->q, a->q_token, a->q_head) && ok(a->q_out, a->qo_token, a->qo_head))) return MTS_EINVAL;
+    if (c.kv_heads && !ok(a->k, a->k_token, a->k_head)) return MTS_EINVAL;
+    if (c.kv_heads && !cached && !ok(a->k_out, a->ko_token, a->ko_head)) return MTS_EINVAL;
+    if (a->v && !ok(a->v, a->v_token, a->v_head)) return MTS_EINVAL;
+    const int64_t e = c.type == MTS_F32 ? 4 : 2;
+    RopeP p;
+    p.q = static_cast<const char*>(a->q);
+    p.k = static_cast<const char*>(a->k);
+    p.v = static_cast<const char*>(a->v);
+    p.qo = static_cast<char*>(a->q_out);
+    p.ko = static_cast<char*>(a->k_out);
+    p.q_token = e * a->q_token, p.q_head = e * a->q_head;
+    p.k_token = e * a->k_token, p.k_head = e * a->k_head;
+    p.v_token = e * a->v_token, p.v_head = e * a->v_head;
+    p.qo_token = e * a->qo_token, p.qo_head = e * a->qo_head;
+    p.ko_token = e * a->ko_token, p.ko_head = e * a->ko_head;
+    p.positions = a->positions;
+    p.freqs = a->freqs;
+    p.slots = a->slots;
+    p.pos = a->pos;
+    p.kc = static_cast<char*>(c.k);
+    p.vc = static_cast<char*>(c.v);
+    p.kc_block = e * c.k_block, p.kc_head = e * c.k_head, p.kc_token = e * c.k_token;
+    p.vc_block = e * c.v_block, p.vc_head = e * c.v_head, p.vc_token = e * c.v_token;
+    p.lb = cached ? int(log2u(c.block_tokens)) : 0;
+    p.n_slots = cached ? int64_t(c.n_blocks) << p.lb : 1;
+    p.q_heads = int(a->q_heads);
+    p.kv_heads = int(c.kv_heads);
+    p.D = int(D);
+    p.rot = int(a->rot);
+    p.n_tokens = int(a->n_tokens);
+    p.mscale = a->mscale;
+    p.sign = a->inverse ? -1.f : 1.f;
+    const bool inter = a->layout == MTS_ROPE_INTERLEAVED;
+    // 16-byte pieces where the rotated part divides into them, single elements else
+    const bool wide = a->rot % (2 * unit) == 0;
+    switch (c.type) {
+    case MTS_BF16: wide ? launch_rope<__bf16, 8>(p, inter, stream) : launch_rope<__bf16, 1>(p, inter, stream); break;
+    case MTS_F16: wide ? launch_rope<_Float16, 8>(p, inter, stream) : launch_rope<_Float16, 1>(p, inter, stream); break;
+    default: wide ? launch_rope<float, 4>(p, inter, stream) : launch_rope<float, 1>(p, inter, stream); break;
+    }
+    return launched();
+}
+
+}  // extern "C"
