@@ -104,7 +104,8 @@ __device__ __forceinline__ void request_tokens(const Batch& b, int r, int& first
 // One job: part `split` of `nsplit` of request r's keys [k0, k1), for KV head
 // hk and one group of its query rows.  `lead` is the id of the split 0 job.
 struct Job {
-    int r, hk, grp, split, nsplit, lead;
+    int id, lead;
+    int r, hk, grp, split, nsplit;
     int L, T, first;
     int k0, k1;
 };
@@ -114,100 +115,117 @@ struct SplitRule {
     int rows;         // query rows (token x head of the group) of a job; 0: all
     int G;            // query heads a KV head
     int target;       // jobs to aim for
+    bool xcd;         // neighbouring jobs (which share keys) to one of the 8 dies
 };
 
-// The jobs of a ragged batch, numbered request by request.  Lengths live on
-// the device, so every workgroup finds its own: it sums the requests' rounds,
-// takes as many rounds a job as leave about `target` jobs, and walks the
-// requests' job counts up to its id.  n / 256 loads a thread.  Returns false
-// for ids past the last job; wave-uniform results.  scratch: 256 threads, 24
-// words of LDS; two barriers a 256 requests and pass.
-__device__ __forceinline__ long long block_sum(long long v, long long* scratch)
+template <int NW>
+__device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* scratch)
 {
     for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
     if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
     __syncthreads();
-    const long long s = scratch[0] + scratch[1] + scratch[2] + scratch[3];
+    int64_t s = 0;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) s += scratch[i];
     __syncthreads();
     return s;
 }
 
-__device__ __forceinline__ bool find_job(const Pool& p, const Batch& b, const SplitRule& s, int id, Job& j, long long* scratch)
+// What one request adds: groups of query rows, rounds over its keys.
+struct Share {
+    int L, T, first, groups, rounds;
+};
+
+__device__ __forceinline__ Share share_of(const Pool& p, const Batch& b, const SplitRule& s, int r)
 {
-    const int t = threadIdx.x;
-    long long rounds = 0;
-    int L = 0, first = 0, T = 0, groups = 0, R = 0;
-    for (int r0 = 0; r0 < b.n; r0 += 256) {
-        const int r = r0 + t;
-        if (r < b.n) {
-            L = request_len(p, b, r);
-            request_tokens(b, r, first, T);
-            groups = s.rows ? int((int64_t(T) * s.G + s.rows - 1) / s.rows) : (T ? 1 : 0);
-            R = L ? (L + s.unit - 1) / s.unit : 1;
-            rounds += (long long)(R)*groups * p.kv_heads;
-        }
+    Share q{0, 0, 0, 0, 1};
+    if (r < b.n) {
+        q.L = request_len(p, b, r);
+        request_tokens(b, r, q.first, q.T);
+        q.groups = s.rows ? int((int64_t(q.T) * s.G + s.rows - 1) / s.rows) : (q.T ? 1 : 0);
+        q.rounds = q.L ? (q.L + s.unit - 1) / s.unit : 1;
     }
-    const long long total = block_sum(rounds, scratch);
+    return q;
+}
+
+// The jobs of a ragged batch, numbered head by head, in it request by request,
+// group by group, split by split.  Lengths live on the device, so every
+// workgroup (NW waves) finds its own job: it sums the requests' rounds, takes
+// as many rounds a job as leave about `target` jobs, and finds its number
+// among the requests' job counts.  One request a thread; more are passed over
+// in turns.  Returns false for numbers past the last job; the results are
+// uniform.  scratch: NW + 4 words of LDS.
+template <int NW>
+__device__ __forceinline__ bool find_job(const Pool& p, const Batch& b, const SplitRule& s, Job& j, int64_t* scratch)
+{
+    constexpr int NT = 64 * NW;
+    const int t = threadIdx.x;
+    Share q{};
+    int64_t rounds = 0;
+    for (int r0 = 0; r0 < b.n; r0 += NT) {
+        q = share_of(p, b, s, r0 + t);
+        rounds += int64_t(q.rounds) * q.groups;
+    }
+    const int64_t total = block_sum<NW>(rounds, scratch) * p.kv_heads;
     const int per = total > s.target ? int((total + s.target - 1) / s.target) : 1;
-    long long before = 0;
-    int* found = reinterpret_cast<int*>(scratch + 8);
-    for (int r0 = 0; r0 < b.n; r0 += 256) {
-        const int r = r0 + t;
-        if (b.n > 256) {
-            groups = 0;
-            R = 1;
-            if (r < b.n) {
-                L = request_len(p, b, r);
-                request_tokens(b, r, first, T);
-                groups = s.rows ? int((int64_t(T) * s.G + s.rows - 1) / s.rows) : (T ? 1 : 0);
-                R = L ? (L + s.unit - 1) / s.unit : 1;
-            }
-        } else if (r >= b.n) {
-            groups = 0;
-            R = 1;
-        }
-        const int ns = (R + per - 1) / per;
-        const long long jobs = (long long)(ns)*groups * p.kv_heads;
-        long long incl = jobs;
+    int64_t mine = 0;
+    for (int r0 = 0; r0 < b.n; r0 += NT) {
+        if (b.n > NT) q = share_of(p, b, s, r0 + t);
+        mine += int64_t((q.rounds + per - 1) / per) * q.groups;
+    }
+    const int64_t head = block_sum<NW>(mine, scratch), jobs = head * p.kv_heads;
+    int64_t id = blockIdx.x;
+    if (s.xcd) {
+        const int64_t chunk = (jobs + 7) / 8;
+        if ((id >> 3) >= chunk) return false;
+        id = (id & 7) * chunk + (id >> 3);
+    }
+    if (id >= jobs) return false;
+    const int hk = int(id / head), in = int(id % head);
+    int* found = reinterpret_cast<int*>(scratch + NW);
+    int64_t before = 0;
+    for (int r0 = 0; r0 < b.n; r0 += NT) {
+        if (b.n > NT) q = share_of(p, b, s, r0 + t);
+        const int ns = (q.rounds + per - 1) / per;
+        const int64_t n = int64_t(ns) * q.groups;
+        int64_t incl = n;
         for (int o = 1; o < 64; o <<= 1) {
-            const long long v = __shfl_up(incl, o);
+            const int64_t v = __shfl_up(incl, o);
             if ((t & 63) >= o) incl += v;
         }
         if ((t & 63) == 63) scratch[t >> 6] = incl;
         if (t == 0) found[0] = -1;
         __syncthreads();
-        long long base = before;
-        for (int w = 0; w < (t >> 6); ++w) base += scratch[w];
-        const long long at = id - (base + incl - jobs);
-        if (at >= 0 && at < jobs) {
-            const int in = int(at);
-            found[0] = r;
-            found[1] = in;
-            found[2] = ns;
-            found[3] = groups;
-            found[4] = L;
-            found[5] = T;
-            found[6] = first;
+        int64_t base = before;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            if (w < (t >> 6)) base += scratch[w];
+            before += scratch[w];
         }
-        before += scratch[0] + scratch[1] + scratch[2] + scratch[3];
+        const int64_t at = in - (base + incl - n);
+        if (at >= 0 && at < n) {
+            found[0] = r0 + t;
+            found[1] = int(at);
+            found[2] = ns;
+            found[3] = q.L;
+            found[4] = q.T;
+            found[5] = q.first;
+        }
         __syncthreads();
         if (found[0] >= 0) break;
     }
+    const int at = __builtin_amdgcn_readfirstlane(found[1]);
+    j.id = int(id);
+    j.hk = hk;
     j.r = __builtin_amdgcn_readfirstlane(found[0]);
-    if (j.r < 0) return false;
-    const int in = __builtin_amdgcn_readfirstlane(found[1]);
     j.nsplit = __builtin_amdgcn_readfirstlane(found[2]);
-    const int grp = __builtin_amdgcn_readfirstlane(found[3]);
-    j.L = __builtin_amdgcn_readfirstlane(found[4]);
-    j.T = __builtin_amdgcn_readfirstlane(found[5]);
-    j.first = __builtin_amdgcn_readfirstlane(found[6]);
-    j.split = in % j.nsplit;
-    j.lead = id - j.split;
-    const int rest = in / j.nsplit;
-    j.grp = rest % grp;
-    j.hk = rest / grp;
-    const long long k0 = (long long)(j.split) * per * s.unit;
-    const long long k1 = k0 + (long long)(per)*s.unit;
+    j.L = __builtin_amdgcn_readfirstlane(found[3]);
+    j.T = __builtin_amdgcn_readfirstlane(found[4]);
+    j.first = __builtin_amdgcn_readfirstlane(found[5]);
+    j.split = at % j.nsplit;
+    j.grp = at / j.nsplit;
+    j.lead = j.id - j.split;
+    const int64_t k0 = int64_t(j.split) * per * s.unit, k1 = k0 + int64_t(per) * s.unit;
     j.k0 = int(k0);
     j.k1 = int(k1 < j.L ? k1 : j.L);
     return true;
@@ -217,7 +235,7 @@ __device__ __forceinline__ bool find_job(const Pool& p, const Batch& b, const Sp
 inline uint64_t max_jobs(uint32_t n, uint64_t n_tokens, uint32_t kv_heads, uint32_t G, uint32_t rows, uint32_t target)
 {
     const uint64_t groups = rows ? n + n_tokens * G / rows : n;
-    return target + groups * kv_heads;
+    return ((target + groups * kv_heads) + 7) / 8 * 8;
 }
 
 }  // namespace ops

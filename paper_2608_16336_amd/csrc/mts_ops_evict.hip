@@ -26,11 +26,11 @@ template <class T, int D>
 __global__ __launch_bounds__(256, 2) void k_weigh(const WeighP p)
 {
     constexpr int KS = D / 32;
-    __shared__ long long scratch[16];
+    __shared__ int64_t scratch[8];
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, lq = lane & 15, c = lane >> 4;
     Job j;
-    const SplitRule rule{kWeighRound, 0, p.G, p.target};
-    if (!find_job(p.pool, p.batch, rule, blockIdx.x, j, scratch)) return;
+    const SplitRule rule{kWeighRound, 0, p.G, p.target, false};
+    if (!find_job<4>(p.pool, p.batch, rule, j, scratch)) return;
     const int rows = j.T * p.G, base = j.L - j.T;
     const char* kh = p.pool.k + int64_t(j.hk) * p.pool.k_head;
     const int omask = (1 << p.pool.lb) - 1;
