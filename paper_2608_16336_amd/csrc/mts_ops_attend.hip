@@ -149,15 +149,24 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_rows(const Att
     const char* vh = p.pool.v + int64_t(j.hk) * p.pool.v_head;
     const int omask = (1 << p.pool.lb) - 1;
 
-    for (int k0 = j.k0 + 32 * w; k0 < j.k1; k0 += kRound) {
-        bool live[2];
-        s16x8 kf[2][KS], vf[2][KS];
+    // the next tile's keys and values are asked for once the present ones have left their registers, the block ids a
+    // tile earlier still
+    int ids[2];
+    bool live[2];
+    s16x8 kf[2][KS], vf[2][KS];
+    const auto load_ids = [&](int k0) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int key = k0 + 16 * u + lq;
-            const int id = key < j.k1 ? block_of(p.pool, p.batch, j.r, key) : -1;
-            live[u] = id >= 0;
-            const int64_t blk = live[u] ? id : 0, off = live[u] ? key & omask : 0;
+            ids[u] = key < j.k1 ? p.batch.table[size_t(j.r) * p.batch.width + (key >> p.pool.lb)] : -1;
+        }
+    };
+    const auto load_tile = [&](int k0) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int key = k0 + 16 * u + lq;
+            live[u] = unsigned(ids[u]) < p.pool.n_blocks;
+            const int64_t blk = live[u] ? ids[u] : 0, off = live[u] ? key & omask : 0;
             const char* kp = kh + blk * p.pool.k_block + off * p.pool.k_token;
             const char* vp = vh + blk * p.pool.v_block + off * p.pool.v_token;
 #pragma unroll
@@ -165,6 +174,14 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_rows(const Att
 #pragma unroll
             for (int s = 0; s < KS; ++s) vf[u][s] = *reinterpret_cast<const s16x8*>(vp + (32 * s + 8 * c) * 2);
         }
+    };
+    int k0 = j.k0 + 32 * w;
+    if (k0 < j.k1) {
+        load_ids(k0);
+        load_tile(k0);
+        load_ids(k0 + kRound);
+    }
+    for (; k0 < j.k1; k0 += kRound) {
         // unseen slots weigh nothing whatever they hold: their values must not reach the product as NaN
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -192,13 +209,21 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_rows(const Att
                 *reinterpret_cast<s16x8*>(&vst[w][row * D * 2 + (((4 * s + c) ^ swz<D>(row)) * 16)]) = vf[u][s];
             }
         lds_order();
+        f32x4 sc[MT][2];
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                sc[m][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int s = 0; s < KS; ++s) sc[m][u] = T::mfma16(kf[u][s], qf[m][s], sc[m][u]);
+            }
+        if (k0 + kRound < j.k1) {
+            load_tile(k0 + kRound);
+            load_ids(k0 + 2 * kRound);
+        }
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            f32x4 sc[2] = {};
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int s = 0; s < KS; ++s) sc[u] = T::mfma16(kf[u][s], qf[m][s], sc[u]);
             float x[8];
             float mx = -__builtin_inff();
 #pragma unroll
@@ -206,7 +231,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_rows(const Att
                 const int in = 4 * c + (i & 3);
                 bool see = (alive[i >> 2] >> in) & 1;
                 if (fresh) see = see && sees(p.batch, j.first + tq[m], tq[m], k0 + 16 * (i >> 2) + in - base);
-                x[i] = see ? sc[i >> 2][i & 3] * p.scale2 : -__builtin_inff();
+                x[i] = see ? sc[m][i >> 2][i & 3] * p.scale2 : -__builtin_inff();
                 mx = fmaxf(mx, x[i]);
             }
             mx = fmaxf(mx, __shfl_xor(mx, 16));

@@ -34,20 +34,44 @@ __global__ __launch_bounds__(256, 2) void k_weigh(const WeighP p)
     const int rows = j.T * p.G, base = j.L - j.T;
     const char* kh = p.pool.k + int64_t(j.hk) * p.pool.k_head;
     const int omask = (1 << p.pool.lb) - 1;
-    for (int k0 = j.k0 + 32 * w; k0 < j.k1; k0 += kWeighRound) {
+    // the next tile's keys are on their way during the present one's rows, their block ids a tile earlier still
+    int ids[2], held[2];
+    s16x8 kn[2][KS];
+    const auto load_ids = [&](int k0) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int key = k0 + 16 * u + lq;
+            ids[u] = key < j.k1 ? p.batch.table[size_t(j.r) * p.batch.width + (key >> p.pool.lb)] : -1;
+        }
+    };
+    const auto load_tile = [&](int k0) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const bool ok = unsigned(ids[u]) < p.pool.n_blocks;
+            held[u] = ok ? ids[u] : -1;
+            const char* kp = kh + int64_t(ok ? ids[u] : 0) * p.pool.k_block + int64_t(ok ? (k0 + 16 * u + lq) & omask : 0) * p.pool.k_token;
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kn[u][s] = *reinterpret_cast<const s16x8*>(kp + (32 * s + 8 * c) * 2);
+        }
+    };
+    int k0 = j.k0 + 32 * w;
+    if (k0 < j.k1) {
+        load_ids(k0);
+        load_tile(k0);
+        load_ids(k0 + kWeighRound);
+    }
+    for (; k0 < j.k1; k0 += kWeighRound) {
         s16x8 kf[2][KS];
         int id[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int key = k0 + 16 * u + lq;
-            id[u] = -1;
-            if (key < j.k1) {
-                const int b = p.batch.table[size_t(j.r) * p.batch.width + (key >> p.pool.lb)];
-                if (unsigned(b) < p.pool.n_blocks) id[u] = b;
-            }
-            const char* kp = kh + int64_t(id[u] < 0 ? 0 : id[u]) * p.pool.k_block + int64_t(id[u] < 0 ? 0 : key & omask) * p.pool.k_token;
+            id[u] = held[u];
 #pragma unroll
-            for (int s = 0; s < KS; ++s) kf[u][s] = *reinterpret_cast<const s16x8*>(kp + (32 * s + 8 * c) * 2);
+            for (int s = 0; s < KS; ++s) kf[u][s] = kn[u][s];
+        }
+        if (k0 + kWeighRound < j.k1) {
+            load_tile(k0 + kWeighRound);
+            load_ids(k0 + 2 * kWeighRound);
         }
         float acc[8] = {};
         const bool fresh = k0 + 32 > base;

@@ -14,11 +14,13 @@ of each request, its new tokens' among them) and q_start [requests + 1] int32
 (first new token of each request).
 """
 import ctypes
+import functools
+import struct
 
 import torch
 
 from . import mts
-from .mts import _check
+from .mts import MtsError, _check
 
 TYPES = {torch.bfloat16: 0, torch.float16: 1, torch.float32: 2}
 LAYOUTS = {"half": 0, "interleaved": 1}
@@ -86,9 +88,8 @@ def _library():
     global _lib
     if _lib is None:
         L = mts.load_library()
-        for name, args in (("mts_rope", mts_rope_args), ("mts_attend", mts_attend_args), ("mts_weigh", mts_weigh_args),
-                           ("mts_evict", mts_evict_args), ("mts_sample", mts_sample_args)):
-            getattr(L, name).argtypes = [ctypes.POINTER(args), _vp]
+        for name in ("mts_rope", "mts_attend", "mts_weigh", "mts_evict", "mts_sample"):
+            getattr(L, name).argtypes = [_vp, _vp]
         L.mts_rope_freqs.argtypes = [_vp, _u32, _f64, _u32, _f64, _f64, _f64, _f64]
         L.mts_attend_workspace.argtypes = [_u32] * 6 + [ctypes.POINTER(_size)]
         L.mts_evict_workspace.argtypes = [_u32] * 5 + [ctypes.POINTER(_size)]
@@ -98,65 +99,89 @@ def _library():
     return _lib
 
 
-def _need(ok, what):
-    if not ok:
-        raise ValueError(what)
+def _packer(cls):
+    """A structure's fields packed in one go: a tenth of the time that setting
+    them one by one takes, which a decode step would wait for."""
+    def codes(c):
+        for _, t in c._fields_:
+            if issubclass(t, ctypes.Structure):
+                yield from codes(t)
+            else:
+                yield {_vp: "P", _u32: "I", _i64: "q", _f32: "f", _size: "N"}[t]
+    s = struct.Struct("@" + "".join(codes(cls)))
+    if ctypes.sizeof(cls) - s.size not in range(8):
+        raise AssertionError(cls)
+    tail = bytes(ctypes.sizeof(cls) - s.size)
+    return (lambda *v: s.pack(*v) + tail) if tail else s.pack
 
 
-def _device(t, what, device, dtype, shape=None):
-    """A contiguous tensor of one type on the call's GPU."""
-    _need(t.device == device and t.dtype == dtype and t.is_contiguous(), "%s: contiguous %s on %s" % (what, dtype, device))
-    _need(shape is None or t.shape == shape, "%s: shape %s, got %s" % (what, shape, tuple(t.shape)))
+_rope_pack, _attend_pack, _weigh_pack, _evict_pack, _sample_pack = (
+    _packer(c) for c in (mts_rope_args, mts_attend_args, mts_weigh_args, mts_evict_args, mts_sample_args))
+_INT32, _INT64, _FLOAT32, _FLOAT64 = torch.int32, torch.int64, torch.float32, torch.float64
+
+
+def _device(t, what, device, dtype, shape):
+    """The address of a contiguous tensor of one type and shape on the call's GPU."""
+    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
+        raise ValueError("%s: contiguous %s %s on %s, got %s %s on %s" % (what, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+    return t.data_ptr()
 
 
 def _rows(t, what, device, dtype):
     """[tokens][heads][dim] with the last dimension contiguous: (token, head) strides."""
-    _need(t.dim() == 3 and t.device == device and t.dtype == dtype and (t.stride(2) == 1 or t.shape[2] == 1),
-          "%s: [tokens][heads][dim] of %s on %s, last dimension contiguous" % (what, dtype, device))
-    return t.stride(0), t.stride(1)
+    s = t.stride()
+    if len(s) != 3 or t.dtype is not dtype or t.device != device or (s[2] != 1 and t.shape[2] != 1):
+        raise ValueError("%s: [tokens][heads][dim] of %s on %s, last dimension contiguous" % (what, dtype, device))
+    return s[0], s[1]
 
 
-def _stream(device):
-    return torch.cuda.current_stream(device).cuda_stream
-
-
-def _fill_pool(P, k_cache, v_cache):
-    c = k_cache
-    _need(c.dim() == 4 and c.stride(3) == 1 and c.dtype in TYPES, "a pool is [blocks][kv_heads][block_tokens][head_dim]")
-    P.k = c.data_ptr()
-    P.k_block, P.k_head, P.k_token = c.stride()[:3]
-    if v_cache is not None:
-        _need(v_cache.shape == c.shape and v_cache.dtype == c.dtype and v_cache.device == c.device and v_cache.stride(3) == 1,
-              "v_cache must match k_cache")
-        P.v = v_cache.data_ptr()
-        P.v_block, P.v_head, P.v_token = v_cache.stride()[:3]
-    P.n_blocks, P.kv_heads, P.block_tokens, P.head_dim = c.shape
-    P.type = TYPES[c.dtype]
-
-
-def _fill_batch(B, device, table, lens, q_start=None, n_tokens=0, max_q=0, tree=None):
-    n = lens.shape[0]
-    _need(table.dim() == 2 and table.shape[0] == n, "table: [requests][width]")
-    _device(table, "table", device, torch.int32)
-    _device(lens, "lens", device, torch.int32, (n,))
-    B.table, B.lens, B.n, B.table_width = table.data_ptr(), lens.data_ptr(), n, table.shape[1]
-    if q_start is not None:
-        _device(q_start, "q_start", device, torch.int32, (n + 1,))
-        B.q_start, B.n_tokens, B.max_q = q_start.data_ptr(), n_tokens, max_q
-    if tree is not None:
-        _need(tree.dim() == 2 and tree.shape[0] == n_tokens, "tree: [tokens][words] int64")
-        _device(tree, "tree", device, torch.int64)
-        B.tree, B.tree_words = tree.data_ptr(), tree.shape[1]
-
-
-def _call(name, args, device):
-    _need(device.type == "cuda", "tensors must be on a GPU")
+def _call(name, packed, device):
+    if device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    fn, i = getattr(_lib or _library(), name), device.index
     # the launch goes to the tensors' GPU, whatever the current one is
-    if device.index == torch.cuda.current_device():
-        _check(name, getattr(_library(), name)(ctypes.byref(args), _stream(device)))
+    if i == torch._C._cuda_getDevice():
+        rc = fn(packed, torch._C._cuda_getCurrentRawStream(i))
     else:
         with torch.cuda.device(device):
-            _check(name, getattr(_library(), name)(ctypes.byref(args), _stream(device)))
+            rc = fn(packed, torch._C._cuda_getCurrentRawStream(i))
+    if rc:
+        raise MtsError(name, rc)
+
+
+def _pool(k, v, device, dtype, heads=None, dim=None):
+    """The fields of a mts_pool."""
+    shape, s = k.shape, k.stride()
+    if len(shape) != 4 or s[3] != 1 or k.dtype not in TYPES:
+        raise ValueError("a pool is [blocks][kv_heads][block_tokens][head_dim] of bfloat16 or float16, last dimension contiguous")
+    if k.device != device or k.dtype is not dtype or (dim is not None and shape[3] != dim) or (heads is not None and shape[1] != heads):
+        raise ValueError("the pool differs from the call's other tensors in heads, head dimension, type or device")
+    at, z = 0, (0, 0, 0)
+    if v is not None:
+        z = v.stride()
+        if v.shape != shape or v.dtype is not dtype or v.device != device or z[3] != 1:
+            raise ValueError("v_cache must match k_cache")
+        at = v.data_ptr()
+    return k.data_ptr(), at, s[0], s[1], s[2], z[0], z[1], z[2], shape[0], shape[2], shape[1], shape[3], TYPES[dtype], 0
+
+
+def _batch(device, table, lens, q_start, n_tokens, max_q, tree):
+    """The fields of a mts_batch."""
+    n = lens.shape[0]
+    if table.dim() != 2:
+        raise ValueError("table: [requests][width]")
+    width, starts, bits, words = table.shape[1], 0, 0, 0
+    if q_start is not None:
+        starts = _device(q_start, "q_start", device, _INT32, (n + 1,))
+        if not 0 <= max_q < 1 << 31:
+            raise ValueError("max_q: %r" % (max_q,))
+    if tree is not None:
+        if tree.dim() != 2:
+            raise ValueError("tree: [tokens][words]")
+        words = tree.shape[1]
+        bits = _device(tree, "tree", device, _INT64, (n_tokens, words))
+    return (_device(table, "table", device, _INT32, (n, width)), _device(lens, "lens", device, _INT32, (n,)), starts, bits, n, width,
+            n_tokens, max_q, words, 0)
 
 
 # ------------------------------------------------------------------ rotary positions
@@ -164,78 +189,75 @@ def _call(name, args, device):
 
 def rope_freqs(rot, base=10000.0, scaling="none", factor=1.0, trained=4096.0, fast=32.0, slow=1.0, device="cuda"):
     """Angles in radians per position of the rot / 2 pairs, float64 (mts_rope_freqs)."""
-    f = torch.empty(rot // 2, dtype=torch.float64)
+    f = torch.empty(max(0, rot) // 2, dtype=torch.float64)
     _check("mts_rope_freqs", _library().mts_rope_freqs(f.data_ptr(), rot, base, SCALINGS[scaling], factor, trained, fast, slow))
     return f.to(device)
 
 
-def _rope_args(q, k, positions, freqs, layout, mscale, inverse):
-    a = mts_rope_args()
+_NO_POOL = (0,) * 8 + (0, 0)
+
+
+def _rope(q, k, v, positions, slots, freqs, pool, pos, layout, mscale, inverse, q_out, k_out):
     any_ = q if q is not None else k
-    _need(any_ is not None, "q or k")
+    if any_ is None:
+        raise ValueError("q or k")
     device, dtype = any_.device, any_.dtype
-    _need(dtype in TYPES, "bfloat16, float16 or float32")
-    n, D = any_.shape[0], any_.shape[2]
-    for x, what in ((q, "q"), (k, "k")):
-        if x is not None:
-            t, h = _rows(x, what, device, dtype)
-            _need(x.shape[0] == n and x.shape[2] == D, "q and k differ in tokens or head dimension")
-            setattr(a, what, x.data_ptr())
-            setattr(a, what + "_token", t)
-            setattr(a, what + "_head", h)
-    _device(positions, "positions", device, torch.int32, (n,))
-    _device(freqs, "freqs", device, torch.float64)
-    _need(freqs.dim() == 1, "freqs: [rot / 2]")
-    a.positions, a.freqs = positions.data_ptr(), freqs.data_ptr()
-    a.n_tokens, a.q_heads, a.rot = n, 0 if q is None else q.shape[1], 2 * freqs.shape[0]
-    a.layout, a.inverse, a.mscale = LAYOUTS[layout], 1 if inverse else 0, mscale
-    a.pool.type, a.pool.head_dim, a.pool.kv_heads = TYPES[dtype], D, 0 if k is None else k.shape[1]
-    return a, device, dtype
-
-
-def _out(x, out, what, a, device, dtype):
-    if x is None:
-        return None
-    if out is None:
-        out = torch.empty(x.shape, dtype=dtype, device=device)
-    t, h = _rows(out, what + "_out", device, dtype)
-    _need(out.shape == x.shape, "%s_out: the shape of %s" % (what, what))
-    setattr(a, what + "_out", out.data_ptr())
-    setattr(a, what + "o_token", t)
-    setattr(a, what + "o_head", h)
-    return out
+    if dtype not in TYPES or any_.dim() != 3:
+        raise ValueError("[tokens][heads][dim] of bfloat16, float16 or float32")
+    n, _, D = any_.shape
+    at, strides = [], []
+    for x, what in ((q, "q"), (k, "k"), (v, "v")):
+        if x is None:
+            at.append(0)
+            strides += (0, 0)
+            continue
+        strides += _rows(x, what, device, dtype)
+        if x.shape[0] != n or x.shape[2] != D:
+            raise ValueError("q, k and v differ in tokens or head dimension")
+        at.append(x.data_ptr())
+    if q is not None and q_out is None:
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if k is not None and k_out is None and slots is None:
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+    for x, y, what in ((q, q_out, "q_out"), (k, k_out, "k_out")):
+        if x is None or y is None:
+            at.append(0)
+            strides += (0, 0)
+            continue
+        strides += _rows(y, what, device, dtype)
+        if y.shape != x.shape:
+            raise ValueError("%s: the shape of its input" % what)
+        at.append(y.data_ptr())
+    if freqs.dim() != 1:
+        raise ValueError("freqs: [rot / 2]")
+    if pool is None:
+        pool = _NO_POOL + (0 if k is None else k.shape[1], D, TYPES[dtype], 0)
+    _call("mts_rope", _rope_pack(
+        *at, *strides, _device(positions, "positions", device, _INT32, (n,)), _device(freqs, "freqs", device, _FLOAT64, freqs.shape),
+        0 if slots is None else _device(slots, "slots", device, _INT64, (n,)), pos, *pool, n, 0 if q is None else q.shape[1],
+        2 * freqs.shape[0], LAYOUTS[layout], 1 if inverse else 0, mscale), device)
+    return q_out, k_out
 
 
 def rope(q, k, positions, freqs, *, layout="half", mscale=1.0, inverse=False, q_out=None, k_out=None):
     """Queries and keys ([tokens][heads][dim], either may be None) turned by
     their positions; returns (q_out, k_out).  inverse turns back, which is
     also the gradient's rotation."""
-    a, device, dtype = _rope_args(q, k, positions, freqs, layout, mscale, inverse)
-    q_out = _out(q, q_out, "q", a, device, dtype)
-    k_out = _out(k, k_out, "k", a, device, dtype)
-    _call("mts_rope", a, device)
-    return q_out, k_out
+    return _rope(q, k, None, positions, None, freqs, None, 0, layout, mscale, inverse, q_out, k_out)
 
 
 def rope_append(q, k, v, positions, slots, freqs, k_cache, v_cache, pos=None, *, layout="half", mscale=1.0, q_out=None):
     """rope() whose keys go to the pool's slots (block * block_tokens + offset,
     int64; -1: nowhere) together with the values and, to pos
     [blocks][kv_heads][block_tokens] int32, the positions; returns q_out."""
-    a, device, dtype = _rope_args(q, k, positions, freqs, layout, mscale, False)
-    q_out = _out(q, q_out, "q", a, device, dtype)
-    _fill_pool(a.pool, k_cache, v_cache)
-    _need(k is not None and k_cache.device == device and k_cache.dtype == dtype and k_cache.shape[3] == k.shape[2]
-          and k_cache.shape[1] == k.shape[1], "k and the pool differ in heads, head dimension, type or device")
-    if v is not None:
-        _need(v.shape == k.shape and v_cache is not None, "v: the shape of k")
-        a.v, (a.v_token, a.v_head) = v.data_ptr(), _rows(v, "v", device, dtype)
-    _device(slots, "slots", device, torch.int64, (k.shape[0],))
-    a.slots = slots.data_ptr()
-    if pos is not None:
-        _device(pos, "pos", device, torch.int32, k_cache.shape[:3])
-        a.pos = pos.data_ptr()
-    _call("mts_rope", a, device)
-    return q_out
+    if k is None or slots is None or k.dim() != 3:
+        raise ValueError("k and slots")
+    if v is not None and (v.shape != k.shape or v_cache is None):
+        raise ValueError("v: the shape of k, and v_cache")
+    device = k.device
+    pool = _pool(k_cache, v_cache, device, k.dtype, k.shape[1], k.shape[2])
+    at = 0 if pos is None else _device(pos, "pos", device, _INT32, k_cache.shape[:3])
+    return _rope(q, k, v, positions, slots, freqs, pool, at, layout, mscale, False, q_out, None)[0]
 
 
 # ------------------------------------------------------------------ attention
@@ -246,16 +268,18 @@ _workspaces = {}
 def _zeroed(device, nbytes):
     """The stream's zero-initialised workspace, grown as needed.  Under graph
     capture a new one from the graph's own memory."""
-    _need(device.type == "cuda", "tensors must be on a GPU")
-    if torch.cuda.is_current_stream_capturing():
+    if device.type != "cuda":
+        raise ValueError("tensors must be on a GPU")
+    if torch._C._cuda_isCurrentStreamCapturing():
         return torch.zeros(nbytes, dtype=torch.uint8, device=device)
-    key = (device.index, _stream(device))
+    key = (device.index, torch._C._cuda_getCurrentRawStream(device.index))
     w = _workspaces.get(key)
     if w is None or w.numel() < nbytes:
         w = _workspaces[key] = torch.zeros(max(nbytes, 1 << 20), dtype=torch.uint8, device=device)
     return w
 
 
+@functools.lru_cache(maxsize=256)
 def attend_workspace(n, n_tokens, max_q, q_heads, kv_heads, head_dim):
     """Bytes of a workspace for attend() calls of at most these sizes."""
     b = _size(0)
@@ -271,27 +295,29 @@ def attend(q, k_cache, v_cache, table, lens, q_start, max_q, *, scale=None, tree
     attend those before them and themselves.  scale: dim ** -0.5 by default.
     workspace: a zeroed uint8 tensor of attend_workspace() bytes kept for one
     stream's calls; by default the module keeps one a stream."""
-    a = mts_attend_args()
     device, dtype = q.device, q.dtype
-    a.q_token, a.q_head = _rows(q, "q", device, dtype)
+    strides = _rows(q, "q", device, dtype)
     N, Hq, D = q.shape
-    _fill_pool(a.pool, k_cache, v_cache)
-    _need(k_cache.device == device and k_cache.dtype == dtype and k_cache.shape[3] == D, "q and the pool differ in head dimension, type or device")
-    _fill_batch(a.batch, device, table, lens, q_start, N, max_q, tree)
+    pool = _pool(k_cache, v_cache, device, dtype, None, D)
+    if v_cache is None:
+        raise ValueError("v_cache")
+    batch = _batch(device, table, lens, q_start, N, max_q, tree)
     if out is None:
         out = torch.empty((N, Hq, D), dtype=dtype, device=device)
-    a.out_token, a.out_head = _rows(out, "out", device, dtype)
-    _need(out.shape == q.shape, "out: the shape of q")
+        outs = (Hq * D, D)
+    else:
+        outs = _rows(out, "out", device, dtype)
+        if out.shape != q.shape:
+            raise ValueError("out: the shape of q")
     if lse is None:
-        lse = torch.empty((N, Hq), dtype=torch.float32, device=device)
-    _device(lse, "lse", device, torch.float32, (N, Hq))
-    a.q, a.out, a.lse, a.q_heads = q.data_ptr(), out.data_ptr(), lse.data_ptr(), Hq
-    a.scale = D ** -0.5 if scale is None else scale
+        lse = torch.empty((N, Hq), dtype=_FLOAT32, device=device)
     if workspace is None:
-        workspace = _zeroed(device, attend_workspace(a.batch.n, N, max_q, Hq, k_cache.shape[1], D))
-    _need(workspace.device == device and workspace.dtype == torch.uint8 and workspace.is_contiguous(), "workspace: uint8 on %s" % device)
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    _call("mts_attend", a, device)
+        workspace = _zeroed(device, attend_workspace(lens.shape[0], N, max_q, Hq, k_cache.shape[1], D))
+    elif workspace.device != device or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous uint8 on %s" % device)
+    _call("mts_attend", _attend_pack(
+        *pool, *batch, q.data_ptr(), out.data_ptr(), _device(lse, "lse", device, _FLOAT32, (N, Hq)), *strides, *outs, Hq,
+        D ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel()), device)
     return out, lse
 
 
@@ -302,19 +328,22 @@ def weigh(q, lse, k_cache, table, lens, q_start, max_q, score, *, scale=None, de
     """Adds to score [blocks][kv_heads][block_tokens] float32 (times decay) the
     softmax weights that every slot gets from the new tokens' queries, lse being
     attend()'s; returns score.  The new tokens' own slots start from zero."""
-    a = mts_weigh_args()
     device, dtype = q.device, q.dtype
-    a.q_token, a.q_head = _rows(q, "q", device, dtype)
+    strides = _rows(q, "q", device, dtype)
     N, Hq, D = q.shape
-    _fill_pool(a.pool, k_cache, None)
-    _need(k_cache.device == device and k_cache.dtype == dtype and k_cache.shape[3] == D, "q and the pool differ in head dimension, type or device")
-    _fill_batch(a.batch, device, table, lens, q_start, N, max_q, tree)
-    _device(lse, "lse", device, torch.float32, (N, Hq))
-    _device(score, "score", device, torch.float32, k_cache.shape[:3])
-    a.q, a.lse, a.score, a.q_heads = q.data_ptr(), lse.data_ptr(), score.data_ptr(), Hq
-    a.scale, a.decay = D ** -0.5 if scale is None else scale, decay
-    _call("mts_weigh", a, device)
+    _call("mts_weigh", _weigh_pack(
+        *_pool(k_cache, None, device, dtype, None, D), *_batch(device, table, lens, q_start, N, max_q, tree), q.data_ptr(),
+        _device(lse, "lse", device, _FLOAT32, (N, Hq)), *strides, _device(score, "score", device, _FLOAT32, k_cache.shape[:3]), Hq,
+        D ** -0.5 if scale is None else scale, decay), device)
     return score
+
+
+@functools.lru_cache(maxsize=256)
+def evict_workspace(n, kv_heads, table_width, block_tokens, budget):
+    """Bytes of the workspace that evict() takes for these sizes."""
+    b = _size(0)
+    _check("mts_evict_workspace", _library().mts_evict_workspace(n, kv_heads, table_width, block_tokens, budget, ctypes.byref(b)))
+    return b.value
 
 
 def evict(k_cache, v_cache, score, pos, table, lens, next_pos, budget, *, recent=0, sink=0, score_out=None, pos_out=None,
@@ -323,29 +352,24 @@ def evict(k_cache, v_cache, score, pos, table, lens, next_pos, budget, *, recent
     first `sink` and last `recent` positions, then the largest scores.  Kept
     rows above the budget move into the holes below it, in the pool, score_out
     and pos_out (by default score and pos themselves); returns the new lens."""
-    a = mts_evict_args()
     device = k_cache.device
-    _fill_pool(a.pool, k_cache, v_cache)
-    _need(v_cache is not None, "v_cache")
-    _fill_batch(a.batch, device, table, lens)
+    pool = _pool(k_cache, v_cache, device, k_cache.dtype)
+    if v_cache is None:
+        raise ValueError("v_cache")
+    if not (0 <= budget < 1 << 32 and 0 <= recent < 1 << 32 and 0 <= sink < 1 << 32):
+        raise ValueError("budget, recent and sink are counts")
+    batch = _batch(device, table, lens, None, 0, 0, None)
     n, shape = lens.shape[0], k_cache.shape[:3]
-    score_out = score if score_out is None else score_out
-    pos_out = pos if pos_out is None else pos_out
-    for t, what, dt in ((score, "score", torch.float32), (score_out, "score_out", torch.float32), (pos, "pos", torch.int32),
-                        (pos_out, "pos_out", torch.int32)):
-        _device(t, what, device, dt, shape)
-    _device(next_pos, "next_pos", device, torch.int32, (n,))
+    s, ps = _device(score, "score", device, _FLOAT32, shape), _device(pos, "pos", device, _INT32, shape)
+    so = s if score_out is None else _device(score_out, "score_out", device, _FLOAT32, shape)
+    po = ps if pos_out is None else _device(pos_out, "pos_out", device, _INT32, shape)
     if lens_out is None:
-        lens_out = torch.empty(n, dtype=torch.int32, device=device)
-    _device(lens_out, "lens_out", device, torch.int32, (n,))
-    b = _size(0)
-    _check("mts_evict_workspace", _library().mts_evict_workspace(n, shape[1], table.shape[1], shape[2], budget, ctypes.byref(b)))
-    workspace = torch.empty(b.value, dtype=torch.uint8, device=device)
-    a.score, a.pos, a.next_pos = score.data_ptr(), pos.data_ptr(), next_pos.data_ptr()
-    a.score_out, a.pos_out, a.lens_out = score_out.data_ptr(), pos_out.data_ptr(), lens_out.data_ptr()
-    a.budget, a.recent, a.sink = budget, recent, sink
-    a.workspace, a.workspace_bytes = workspace.data_ptr(), b.value
-    _call("mts_evict", a, device)
+        lens_out = torch.empty(n, dtype=_INT32, device=device)
+    nbytes = evict_workspace(n, shape[1], table.shape[1], shape[2], budget)
+    workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    _call("mts_evict", _evict_pack(
+        *pool, *batch, s, ps, _device(next_pos, "next_pos", device, _INT32, (n,)), so, po, _device(lens_out, "lens_out", device, _INT32, (n,)),
+        budget, recent, sink, 0, workspace.data_ptr(), nbytes), device)
     return lens_out
 
 
@@ -357,21 +381,17 @@ def sample(logits, u, temperature, top_k, top_p, min_p, *, token=None, logprob=N
     u [rows]; returns (token int32, logprob float32).  temperature 0 is greedy;
     top_k 0, top_p 1 and min_p 0 keep everything.  A row without a logit above
     -inf gives token -1."""
-    _need(logits.dim() == 2 and logits.dtype in TYPES and (logits.stride(1) == 1 or logits.shape[1] == 1),
-          "logits: [rows][vocab], rows contiguous")
-    device, rows = logits.device, logits.shape[0]
-    a = mts_sample_args()
-    for t, what, dt in ((u, "u", torch.float32), (temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32),
-                        (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32)):
-        _device(t, what, device, dt, (rows,))
-        setattr(a, what, t.data_ptr())
+    if logits.dim() != 2 or logits.dtype not in TYPES or (logits.stride(1) != 1 and logits.shape[1] != 1):
+        raise ValueError("logits: [rows][vocab] of bfloat16, float16 or float32, rows contiguous")
+    device, (rows, vocab) = logits.device, logits.shape
     if token is None:
-        token = torch.empty(rows, dtype=torch.int32, device=device)
+        token = torch.empty(rows, dtype=_INT32, device=device)
     if logprob is None:
-        logprob = torch.empty(rows, dtype=torch.float32, device=device)
-    _device(token, "token", device, torch.int32, (rows,))
-    _device(logprob, "logprob", device, torch.float32, (rows,))
-    a.logits, a.row_stride, a.rows, a.vocab, a.type = logits.data_ptr(), logits.stride(0), rows, logits.shape[1], TYPES[logits.dtype]
-    a.token, a.logprob = token.data_ptr(), logprob.data_ptr()
-    _call("mts_sample", a, device)
+        logprob = torch.empty(rows, dtype=_FLOAT32, device=device)
+    one = (rows,)
+    _call("mts_sample", _sample_pack(
+        logits.data_ptr(), logits.stride(0), _device(u, "u", device, _FLOAT32, one), _device(temperature, "temperature", device, _FLOAT32, one),
+        _device(top_k, "top_k", device, _INT32, one), _device(top_p, "top_p", device, _FLOAT32, one),
+        _device(min_p, "min_p", device, _FLOAT32, one), _device(token, "token", device, _INT32, one),
+        _device(logprob, "logprob", device, _FLOAT32, one), rows, vocab, TYPES[logits.dtype], 0), device)
     return token, logprob
