@@ -21,7 +21,8 @@
  * host: kernels clamp lengths to the table and token ranges to the arrays
  * (q_start must not fall), and a block id outside the pool makes its slots
  * unattended, unweighed, unwritten.  Strides are in elements.  Tensors of 16-bit types need 16-byte
- * aligned pointers and strides that are multiples of 8 (mts_sample: none).
+ * aligned pointers and strides that are multiples of 8 below 2^35 (mts_sample:
+ * none).
  */
 #ifndef MTS_OPS_H
 #define MTS_OPS_H
@@ -122,12 +123,11 @@ typedef struct mts_attend_args {
     int64_t q_token, q_head, out_token, out_head;
     uint32_t q_heads;             /* a multiple of kv_heads */
     float scale;
-    void* workspace;              /* at least mts_attend_workspace bytes, 256-byte aligned.  Zero before its first use; calls
-                                     leave it so that the next one in stream order can use it, whatever its sizes */
-    size_t workspace_bytes;       /* the same for every call with this workspace */
+    void* workspace;              /* mts_attend_workspace bytes, 256-byte aligned, of any contents */
+    size_t workspace_bytes;
 } mts_attend_args;
 int mts_attend(const mts_attend_args* args, hipStream_t stream);
-/* Bytes for calls of at most these sizes. */
+/* Bytes of the workspace of a call of these sizes. */
 int mts_attend_workspace(uint32_t n, uint32_t n_tokens, uint32_t max_q, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim,
                          size_t* bytes);
 

@@ -1,8 +1,16 @@
 // Attention of new tokens over a paged cache (mts_attend).
+#include <type_traits>
+
 #include "mts_ops_dev.h"
 
 namespace mts {
 namespace ops {
+
+// A split 0 job's rows; nsplit is 0 in the others' records.
+struct Part {
+    int nsplit, step, rows, row0, hk, first;
+    int pad[2];
+};
 
 struct AttendP {
     Pool pool;
@@ -13,7 +21,8 @@ struct AttendP {
     int64_t q_token, q_head, out_token, out_head;  // bytes
     int G, q_heads;
     float scale2;  // scale * log2 e: the softmax runs in powers of two
-    unsigned* count;
+    int* jobs;       // how many jobs there are
+    Part* part;      // [job] what k_attend_join has to know of it
     float* part_ml;  // [job][rows][2] running maximum and sum
     float* part_o;   // [job][rows][D]
     int target;
@@ -28,15 +37,6 @@ __device__ __forceinline__ int block_of(const Pool& p, const Batch& b, int r, in
     return unsigned(id) < p.n_blocks ? id : -1;
 }
 
-// 16-byte pieces of a staged row are swapped by row so that the transposed
-// reads of 16 rows fall on different banks.
-template <int D>
-__device__ __forceinline__ int swz(int row)
-{
-    constexpr int CH = D / 8;
-    return CH % 16 == 0 ? (row & 15) : CH % 8 == 0 ? ((row >> 1) & 7) : ((row >> 2) & 3);
-}
-
 // Whether new token t of a request may see slot j at offset rel = j - (L - T) among the new ones.
 __device__ __forceinline__ bool sees(const Batch& b, int tok, int t, int rel)
 {
@@ -45,53 +45,51 @@ __device__ __forceinline__ bool sees(const Batch& b, int tok, int t, int rel)
     return rel < 64 * b.words && ((b.tree[size_t(tok) * b.words + (rel >> 6)] >> (rel & 63)) & 1);
 }
 
-// Joins the parts of a job's rows, in the order of the splits, once the last
-// of its workgroups has written its own: partial sums o, maxima m (in powers
-// of two) and sums l of the waves or the splits.
-//
-// The softmax of a row over parts: o = sum_i 2^(m_i - M) o_i, l likewise.
+// One row's output and lse from its sum o of weighted values, maximum M (in powers of two) and sum of weights l.
 template <class T, int D>
-__device__ __forceinline__ void store_row(const AttendP& p, const Job& j, int row, int d, f32x4 o, float M, float l)
+__device__ __forceinline__ void store_row(const AttendP& p, int hk, int first, int row, int d, f32x4 o, float M, float l)
 {
-    const int t = row / p.G, h = j.hk * p.G + row % p.G;
-    const size_t tok = size_t(j.first) + t;
+    const int t = row / p.G, h = hk * p.G + row % p.G;
+    const size_t tok = size_t(first) + t;
     const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : l);  // a NaN sum stays one
     *reinterpret_cast<s16x4*>(p.out + tok * p.out_token + int64_t(h) * p.out_head + 2 * d) = pack4<T>(o * inv);
     if (d == 0 && p.lse) p.lse[tok * p.q_heads + h] = l == 0.f ? -__builtin_inff() : M * kLn2 + __logf(l);
 }
 
-// Called by every thread of a job of several splits after it has written its
-// part: the last of the splits' workgroups joins them, in their order.  The
-// counter's fences make the others' parts visible to it across the dies.
-template <class T, int D, int NT>
-__device__ __forceinline__ void join_splits(const AttendP& p, const Job& j, int row0, int rows, int RG, int* last)
+// What the joining kernel reads of a job; one thread writes it.
+__device__ __forceinline__ void record_part(const AttendP& p, const Job& j, int64_t jobs, int row0, int rows)
 {
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        const unsigned before = __hip_atomic_fetch_add(&p.count[j.lead], 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        *last = before + 1 == unsigned(j.nsplit);
-        if (*last) {
-            p.count[j.lead] = 0;
-            __threadfence();
-        }
-    }
-    __syncthreads();
-    if (!*last) return;
-    for (int e = threadIdx.x; e < rows * (D / 4); e += NT) {
+    if (threadIdx.x) return;
+    if (j.id == 0) *p.jobs = int(jobs);
+    p.part[j.id] = Part{j.split == 0 ? j.nsplit : 0, j.step, rows, row0, j.hk, j.first, {}};
+}
+
+// Joins the splits of rows whose keys several jobs shared, in their order:
+// with M the largest of the parts' maxima, o = sum_i 2^(m_i - M) o_i and l
+// likewise.  A kernel of its own: the fences that let the last workgroup of a
+// row join in the same launch write back a die's whole cache, and a decode of
+// 150 requests took 115 us with them, 1.2 ms at eight times the splits.
+template <class T, int D>
+__global__ __launch_bounds__(256) void k_attend_join(const AttendP p, const int RG)
+{
+    if (int(blockIdx.x) >= *p.jobs) return;
+    const Part q = p.part[blockIdx.x];
+    if (q.nsplit < 2) return;
+    for (int e = blockIdx.y * 256 + threadIdx.x; e < q.rows * (D / 4); e += 256 * gridDim.y) {
         const int row = e / (D / 4), d = 4 * (e % (D / 4));
+        const size_t at = size_t(blockIdx.x) * RG + row;
         float M = -__builtin_inff();
-        for (int i = 0; i < j.nsplit; ++i) M = fmaxf(M, p.part_ml[2 * (size_t(j.lead + i) * RG + row)]);
+        for (int i = 0; i < q.nsplit; ++i) M = fmaxf(M, p.part_ml[2 * (at + size_t(i) * q.step * RG)]);
         const float ref = M == -__builtin_inff() ? 0.f : M;
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
         float ls = 0.f;
-        for (int i = 0; i < j.nsplit; ++i) {
-            const size_t at = size_t(j.lead + i) * RG + row;
-            const float f = exp2_fast(p.part_ml[2 * at] - ref);
-            s += f * *reinterpret_cast<const f32x4*>(&p.part_o[at * D + d]);
-            ls += f * p.part_ml[2 * at + 1];
+        for (int i = 0; i < q.nsplit; ++i) {
+            const size_t k = at + size_t(i) * q.step * RG;
+            const float f = exp2_fast(p.part_ml[2 * k] - ref);
+            s += f * *reinterpret_cast<const f32x4*>(&p.part_o[k * D + d]);
+            ls += f * p.part_ml[2 * k + 1];
         }
-        store_row<T, D>(p, j, row0 + row, d, s, M, ls);
+        store_row<T, D>(p, q.hk, q.first, q.row0 + row, d, s, M, ls);
     }
 }
 
@@ -111,464 +109,535 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_rows(const Att
     __shared__ float wm[4][16], wl[4][16];
     __shared__ float pst[4][32 * 17];
     __shared__ int64_t scratch[8];
-    __shared__ int last;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, lq = lane & 15, c = lane >> 4;
+    const SplitRule rule{kRound, RG, p.G, p.target};
+    Jobs<4> all(p.pool, p.batch, rule, scratch);
     Job j;
-    const SplitRule rule{kRound, RG, p.G, p.target, false};
-    if (!find_job<4>(p.pool, p.batch, rule, j, scratch)) return;
-    const int rows = min(RG, j.T * p.G - j.grp * RG), row0 = j.grp * RG;
-    const int base = j.L - j.T;
+    for (int turn = 0; all.get(turn, j); ++turn) {
+        // held: what follows from the lane stays in the job
+        const int tid = held(threadIdx.x, turn), lane = tid & 63, w = uniform(tid >> 6), lq = lane & 15, c = lane >> 4;
+        const int rows = min(RG, j.T * p.G - j.grp * RG), row0 = j.grp * RG;
+        const int base = j.L - j.T;
+        record_part(p, j, all.jobs, row0, rows);
 
-    s16x8 qf[MT][KS];
-    int tq[MT];
+        s16x8 qf[MT][KS];
+        int tq[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        const int row = 16 * m + lq;
-        const bool ok = row < rows;
-        const int rr = row0 + (ok ? row : 0);
-        tq[m] = rr / p.G;
-        const char* qp = p.q + (size_t(j.first) + tq[m]) * p.q_token + int64_t(j.hk * p.G + rr % p.G) * p.q_head;
+        for (int m = 0; m < MT; ++m) {
+            const int row = 16 * m + lq;
+            const bool ok = row < rows;
+            const int rr = row0 + (ok ? row : 0);
+            tq[m] = rr / p.G;
+            const char* qp = p.q + (size_t(j.first) + tq[m]) * p.q_token + int64_t(j.hk * p.G + rr % p.G) * p.q_head;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) {
-            const s16x8 x = *reinterpret_cast<const s16x8*>(qp + (32 * s + 8 * c) * 2);
-            qf[m][s] = ok ? x : s16x8{};
+            for (int s = 0; s < KS; ++s) {
+                const s16x8 x = *reinterpret_cast<const s16x8*>(qp + (32 * s + 8 * c) * 2);
+                qf[m][s] = ok ? x : s16x8{};
+            }
+            settle(qf[m]);
         }
-    }
 
-    f32x4 o[MT][DT];
-    float m_run[MT], l_run[MT];
+        f32x4 o[MT][DT];
+        float m_run[MT], l_run[MT];
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        m_run[m] = -__builtin_inff();
-        l_run[m] = 0.f;
+        for (int m = 0; m < MT; ++m) {
+            m_run[m] = -__builtin_inff();
+            l_run[m] = 0.f;
 #pragma unroll
-        for (int t = 0; t < DT; ++t) o[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-
-    const char* kh = p.pool.k + int64_t(j.hk) * p.pool.k_head;
-    const char* vh = p.pool.v + int64_t(j.hk) * p.pool.v_head;
-    const int omask = (1 << p.pool.lb) - 1;
-
-    // the next tile's keys and values are asked for once the present ones have left their registers, the block ids a
-    // tile earlier still
-    int ids[2];
-    bool live[2];
-    s16x8 kf[2][KS], vf[2][KS];
-    const auto load_ids = [&](int k0) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int key = k0 + 16 * u + lq;
-            ids[u] = key < j.k1 ? p.batch.table[size_t(j.r) * p.batch.width + (key >> p.pool.lb)] : -1;
+            for (int t = 0; t < DT; ++t) o[m][t] = f32x4{0.f, 0.f, 0.f, 0.f};
         }
-    };
-    const auto load_tile = [&](int k0) {
+
+        const char* kh = head_of(p.pool.k, p.pool.k_head, j.hk);
+        const char* vh = head_of(p.pool.v, p.pool.v_head, j.hk);
+        const int omask = (1 << p.pool.lb) - 1;
+
+        // the next tile's keys and values are asked for once the present ones have left their registers, the block ids a
+        // tile earlier still
+        int ids[2];
+        bool live[2];
+        s16x8 kf[2][KS], vf[2][KS];
+        const auto load_ids = [&](int k0) {
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int key = k0 + 16 * u + lq;
-            live[u] = unsigned(ids[u]) < p.pool.n_blocks;
-            const int64_t blk = live[u] ? ids[u] : 0, off = live[u] ? key & omask : 0;
-            const char* kp = kh + blk * p.pool.k_block + off * p.pool.k_token;
-            const char* vp = vh + blk * p.pool.v_block + off * p.pool.v_token;
+            for (int u = 0; u < 2; ++u) {
+                const int key = k0 + 16 * u + lq;
+                ids[u] = key < j.k1 ? p.batch.table[size_t(j.r) * p.batch.width + (key >> p.pool.lb)] : -1;
+            }
+        };
+        const auto load_tile = [&](int k0) {
 #pragma unroll
-            for (int s = 0; s < KS; ++s) kf[u][s] = *reinterpret_cast<const s16x8*>(kp + (32 * s + 8 * c) * 2);
+            for (int u = 0; u < 2; ++u) {
+                const int key = k0 + 16 * u + lq;
+                live[u] = unsigned(ids[u]) < p.pool.n_blocks;
+                const int blk = live[u] ? ids[u] : 0, off = live[u] ? key & omask : 0;
+                const char* kp = row_of(kh, p.pool.k_block, p.pool.k_token, blk, off);
+                const char* vp = row_of(vh, p.pool.v_block, p.pool.v_token, blk, off);
 #pragma unroll
-            for (int s = 0; s < KS; ++s) vf[u][s] = *reinterpret_cast<const s16x8*>(vp + (32 * s + 8 * c) * 2);
+                for (int s = 0; s < KS; ++s) kf[u][s] = *reinterpret_cast<const s16x8*>(kp + (32 * s + 8 * c) * 2);
+#pragma unroll
+                for (int s = 0; s < KS; ++s) vf[u][s] = *reinterpret_cast<const s16x8*>(vp + (32 * s + 8 * c) * 2);
+            }
+        };
+        int k0 = j.k0 + 32 * w;
+        if (k0 < j.k1) {
+            load_ids(k0);
+            load_tile(k0);
+            load_ids(k0 + kRound);
         }
-    };
-    int k0 = j.k0 + 32 * w;
-    if (k0 < j.k1) {
-        load_ids(k0);
-        load_tile(k0);
-        load_ids(k0 + kRound);
-    }
-    for (; k0 < j.k1; k0 += kRound) {
-        // unseen slots weigh nothing whatever they hold: their values must not reach the product as NaN
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int s = 0; s < KS; ++s)
-                if (!live[u]) vf[u][s] = s16x8{};
-        const unsigned long long alive[2] = {__ballot(live[0]) & 0xffff, __ballot(live[1]) & 0xffff};
-        const bool fresh = k0 + 32 > base;  // some of these slots are new tokens': rows differ in what they see
-        bool odd = false;
-        if (fresh) {
+        for (; k0 < j.k1; k0 += kRound) {
+            // unseen slots weigh nothing whatever they hold: their values must not reach the product as NaN
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int s = 0; s < KS; ++s)
+                    if (!live[u]) vf[u][s] = s16x8{};
+            const unsigned long long alive[2] = {__ballot(live[0]) & 0xffff, __ballot(live[1]) & 0xffff};
+            const bool fresh = k0 + 32 > base;  // some of these slots are new tokens': rows differ in what they see
+            bool odd = false;
+            if (fresh) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) odd |= (unsigned(vf[u][s][i]) & T::kExp) == T::kExp;
-            odd = __any(odd);
-        }
-        lds_order();
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+                    for (int s = 0; s < KS; ++s)
 #pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const int row = 16 * u + lq;
-                *reinterpret_cast<s16x8*>(&vst[w][row * D * 2 + (((4 * s + c) ^ swz<D>(row)) * 16)]) = vf[u][s];
+                        for (int i = 0; i < 8; ++i) odd |= (unsigned(vf[u][s][i]) & T::kExp) == T::kExp;
+                odd = __any(odd);
             }
-        lds_order();
-        f32x4 sc[MT][2];
+            lds_order();
 #pragma unroll
-        for (int m = 0; m < MT; ++m)
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                sc[m][u] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int s = 0; s < KS; ++s) sc[m][u] = T::mfma16(kf[u][s], qf[m][s], sc[m][u]);
-            }
-        if (k0 + kRound < j.k1) {
-            load_tile(k0 + kRound);
-            load_ids(k0 + 2 * kRound);
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-            float x[8];
-            float mx = -__builtin_inff();
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const int in = 4 * c + (i & 3);
-                bool see = (alive[i >> 2] >> in) & 1;
-                if (fresh) see = see && sees(p.batch, j.first + tq[m], tq[m], k0 + 16 * (i >> 2) + in - base);
-                x[i] = see ? sc[m][i >> 2][i & 3] * p.scale2 : -__builtin_inff();
-                mx = fmaxf(mx, x[i]);
-            }
-            mx = fmaxf(mx, __shfl_xor(mx, 16));
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const float mn = fmaxf(m_run[m], mx);
-            const float ref = mn == -__builtin_inff() ? 0.f : mn;
-            const float alpha = exp2_fast(m_run[m] - ref);
-            m_run[m] = mn;
-            f32x8 pr;
-            float sum = 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                pr[i] = exp2_fast(x[i] - ref);
-                sum += pr[i];
-            }
-            l_run[m] = l_run[m] * alpha + sum;
-#pragma unroll
-            for (int t = 0; t < DT; ++t) o[m][t] *= alpha;
-            if (!odd) {
-                const s16x8 pf = pack8<T>(pr);
-#pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    s16x8 a;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int row = 16 * u + 4 * c + (lq >> 2), piece = 2 * t + ((lq & 3) >> 1);
-                        const s16x4 x4 = read_tr16(&vst[w][row * D * 2 + ((piece ^ swz<D>(row)) * 16) + (lq & 1) * 8]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) a[4 * u + i] = x4[i];
-                    }
-                    o[m][t] = T::mfma16(a, pf, o[m][t]);
+                for (int s = 0; s < KS; ++s) {
+                    const int row = 16 * u + lq;
+                    *reinterpret_cast<s16x8*>(&vst[w][row * D * 2 + (((4 * s + c) ^ swz_tr16<D>(row)) * 16)]) = vf[u][s];
                 }
-            } else {
-                // infinities or NaN among the new tokens' values: only the rows that see a slot take its value
-                lds_order();
+            lds_order();
+            f32x4 sc[MT][2];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) pst[w][(16 * (i >> 2) + 4 * c + (i & 3)) * 17 + lq] = x[i] == -__builtin_inff() ? -1.f : pr[i];
-                lds_order();
-                for (int key = 0; key < 32; ++key) {
-                    const float pk = pst[w][key * 17 + lq];
-                    if (pk < 0.f) continue;
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    sc[m][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 0; s < KS; ++s) sc[m][u] = T::mfma16(kf[u][s], qf[m][s], sc[m][u]);
+                }
+            if (k0 + kRound < j.k1) {
+                load_tile(k0 + kRound);
+                load_ids(k0 + 2 * kRound);
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+                float x[8];
+                float mx = -__builtin_inff();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int in = 4 * c + (i & 3);
+                    bool see = (alive[i >> 2] >> in) & 1;
+                    if (fresh) see = see && sees(p.batch, j.first + tq[m], tq[m], k0 + 16 * (i >> 2) + in - base);
+                    x[i] = see ? sc[m][i >> 2][i & 3] * p.scale2 : -__builtin_inff();
+                    mx = fmaxf(mx, x[i]);
+                }
+                mx = fmaxf(mx, __shfl_xor(mx, 16));
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                const float mn = fmaxf(m_run[m], mx);
+                const float ref = mn == -__builtin_inff() ? 0.f : mn;
+                const float alpha = exp2_fast(m_run[m] - ref);
+                m_run[m] = mn;
+                f32x8 pr;
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    pr[i] = exp2_fast(x[i] - ref);
+                    sum += pr[i];
+                }
+                l_run[m] = l_run[m] * alpha + sum;
+#pragma unroll
+                for (int t = 0; t < DT; ++t) o[m][t] *= alpha;
+                if (!odd) {
+                    const s16x8 pf = pack8<T>(pr);
 #pragma unroll
                     for (int t = 0; t < DT; ++t) {
-                        const int d = 16 * t + 4 * c;
-                        const s16x4 v4 = *reinterpret_cast<const s16x4*>(&vst[w][key * D * 2 + (((d >> 3) ^ swz<D>(key)) * 16) + (d & 4) * 2]);
+                        s16x8 a;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) o[m][t][i] += pk * widen<T>(v4[i]);
+                        for (int u = 0; u < 2; ++u) {
+                            const int row = 16 * u + 4 * c + (lq >> 2), piece = 2 * t + ((lq & 3) >> 1);
+                            const s16x4 x4 = read_tr16(&vst[w][row * D * 2 + ((piece ^ swz_tr16<D>(row)) * 16) + (lq & 1) * 8]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) a[4 * u + i] = x4[i];
+                        }
+                        o[m][t] = T::mfma16(a, pf, o[m][t]);
+                    }
+                } else {
+                    // infinities or NaN among the new tokens' values: only the rows that see a slot take its value
+                    lds_order();
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) pst[w][(16 * (i >> 2) + 4 * c + (i & 3)) * 17 + lq] = x[i] == -__builtin_inff() ? -1.f : pr[i];
+                    lds_order();
+                    for (int key = 0; key < 32; ++key) {
+                        const float pk = pst[w][key * 17 + lq];
+                        if (pk < 0.f) continue;
+#pragma unroll
+                        for (int t = 0; t < DT; ++t) {
+                            const int d = 16 * t + 4 * c;
+                            const s16x4 v4 = *reinterpret_cast<const s16x4*>(&vst[w][key * D * 2 + (((d >> 3) ^ swz_tr16<D>(key)) * 16) + (d & 4) * 2]);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[m][t][i] += pk * widen<T>(v4[i]);
+                        }
+                    }
+                    lds_order();
+                }
+            }
+        }
+
+        // the four waves' rows joined, 16 at a time
+        const bool whole = j.nsplit == 1;
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float l = l_run[m];
+            l += __shfl_xor(l, 16);
+            l += __shfl_xor(l, 32);
+            __syncthreads();
+            if (c == 0) {
+                wm[w][lq] = m_run[m];
+                wl[w][lq] = l;
+            }
+            float* mine = reinterpret_cast<float*>(vst[w]);
+#pragma unroll
+            for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(&mine[lq * D + 16 * t + 4 * c]) = o[m][t];
+            __syncthreads();
+            for (int e = tid; e < 16 * (D / 4); e += 256) {
+                const int row = e / (D / 4), d = 4 * (e % (D / 4));
+                if (16 * m + row >= rows) break;
+                float M = fmaxf(fmaxf(wm[0][row], wm[1][row]), fmaxf(wm[2][row], wm[3][row]));
+                const float ref = M == -__builtin_inff() ? 0.f : M;
+                f32x4 s = {0.f, 0.f, 0.f, 0.f};
+                float ls = 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float f = exp2_fast(wm[i][row] - ref);
+                    s += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(vst[i]) + row * D + d);
+                    ls += f * wl[i][row];
+                }
+                if (whole) {
+                    store_row<T, D>(p, j.hk, j.first, row0 + 16 * m + row, d, s, M, ls);
+                } else {
+                    const size_t at = size_t(j.id) * RG + 16 * m + row;
+                    *reinterpret_cast<f32x4*>(&p.part_o[at * D + d]) = s;
+                    if (d == 0) {
+                        p.part_ml[2 * at] = M;
+                        p.part_ml[2 * at + 1] = ls;
                     }
                 }
-                lds_order();
             }
         }
     }
-
-    // the four waves' rows joined, 16 at a time
-    const bool whole = j.nsplit == 1;
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-        float l = l_run[m];
-        l += __shfl_xor(l, 16);
-        l += __shfl_xor(l, 32);
-        __syncthreads();
-        if (c == 0) {
-            wm[w][lq] = m_run[m];
-            wl[w][lq] = l;
-        }
-        float* mine = reinterpret_cast<float*>(vst[w]);
-#pragma unroll
-        for (int t = 0; t < DT; ++t) *reinterpret_cast<f32x4*>(&mine[lq * D + 16 * t + 4 * c]) = o[m][t];
-        __syncthreads();
-        for (int e = threadIdx.x; e < 16 * (D / 4); e += 256) {
-            const int row = e / (D / 4), d = 4 * (e % (D / 4));
-            if (16 * m + row >= rows) break;
-            float M = fmaxf(fmaxf(wm[0][row], wm[1][row]), fmaxf(wm[2][row], wm[3][row]));
-            const float ref = M == -__builtin_inff() ? 0.f : M;
-            f32x4 s = {0.f, 0.f, 0.f, 0.f};
-            float ls = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float f = exp2_fast(wm[i][row] - ref);
-                s += f * *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(vst[i]) + row * D + d);
-                ls += f * wl[i][row];
-            }
-            if (whole) {
-                store_row<T, D>(p, j, row0 + 16 * m + row, d, s, M, ls);
-            } else {
-                const size_t at = size_t(j.id) * RG + 16 * m + row;
-                *reinterpret_cast<f32x4*>(&p.part_o[at * D + d]) = s;
-                if (d == 0) {
-                    p.part_ml[2 * at] = M;
-                    p.part_ml[2 * at + 1] = ls;
-                }
-            }
-        }
-    }
-    if (whole) return;
-
-    join_splits<T, D, 256>(p, j, row0, rows, RG, &last);
 }
 
-// Many query rows: tiles of 64 or 32 keys shared by the waves, 32 rows a wave.
+// Many query rows: tiles of 64 keys shared by the waves, 32 rows a wave.
 //
-// The tile after next's block ids and the next tile's keys and values are on
-// their way to registers while the waves compute the present one from LDS;
-// two tiles take turns there.  As in the other kernel scores are S^T = K Q^T,
-// here 32 x 32, and a lane holds 32 scores of one query: their layout is that
-// of P^T in O^T += V^T P^T, with V^T from transposed reads.  The running
-// maximum is only followed when it grew by more than 2^kSlack since the sums
-// were last scaled (weights up to 2^kSlack lose nothing in 32 bits nor in the
-// rounding to 16).
+// As in the other kernel scores are S^T = K Q^T, here 32 x 32, and a lane holds
+// 16 scores of one query for each half of a tile: their layout is that of P^T
+// in O^T += V^T P^T, with V^T from transposed reads.  The matrix products and
+// the softmax take about as long as each other, so three halves are under way
+// at once: the scores of the next one and the values of the last one are
+// multiplied while the present one's weights are formed, none of which waits
+// for another.
+//
+// A tile's keys and values go through registers to LDS, two tiles of each in
+// turn.  The keys of tile i + 1 and the values of tile i are stored when round
+// i begins: the buffers they replace were last read before the barrier in the
+// middle of round i - 1, the only one of a round.  Loads run a round ahead of
+// the stores, block ids one more.
+//
+// The running maximum is only followed when it grew by more than 2^kSlack
+// since the sums were last scaled (weights up to 2^kSlack lose nothing in 32
+// bits nor in the rounding to 16).
 //
 // Values of new tokens that are not finite cannot go through the product,
 // where rows that do not see them would take 0 x inf: they are staged as zero
 // and added to the rows that see them, which is what weighting them gives.
 constexpr float kSlack = 8.f;
-// keys of a tile: half as many where a row is twice as long
-constexpr int tile_keys(int D) { return D == 256 ? 32 : 64; }
+constexpr float kLowest = -3.0e38f;  // below any score's power of two
+
+template <int N>
+using Int = std::integral_constant<int, N>;
 
 template <class T, int D, int NW>
 __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void k_attend_tiles(const AttendP p)
 {
-    constexpr int NT = 64 * NW, RG = 32 * NW, CH = D / 8, KS = D / 16, DT = D / 32, kTile = tile_keys(D), UT = kTile / 32;
-    constexpr int PIECES = (kTile * CH + NT - 1) / NT;  // 16-byte pieces a thread stages of each of K and V, at most
-    constexpr bool EVEN = kTile * CH % NT == 0;
+    constexpr int NT = 64 * NW, RG = 32 * NW, CH = D / 8, KS = D / 16, DT = D / 32, kTile = 64;
+    // a thread stages PIECES 16-byte pieces of one row, NW apart, of the keys and of the values
+    constexpr int PIECES = (CH + NW - 1) / NW;
+    constexpr bool EVEN = CH % NW == 0;
     __shared__ __attribute__((aligned(16))) char ks[2][kTile * D * 2];
     __shared__ __attribute__((aligned(16))) char vs[2][kTile * D * 2];
     __shared__ int64_t scratch[NW + 4];
-    __shared__ int last;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, lq = lane & 31, h = lane >> 5;
+    const SplitRule rule{kTile, RG, p.G, p.target};
+    Jobs<NW> all(p.pool, p.batch, rule, scratch);
     Job j;
-    const SplitRule rule{64, RG, p.G, p.target, true};
-    if (!find_job<NW>(p.pool, p.batch, rule, j, scratch)) return;
-    const int row0 = j.grp * RG, rows = min(RG, j.T * p.G - row0), base = j.L - j.T;
-    // a chain's later slots are seen by none of the group's rows
-    if (!p.batch.tree) j.k1 = min(j.k1, base + (row0 + rows - 1) / p.G + 1);
+    for (int turn = 0; all.get(turn, j); ++turn) {
+        // held: what follows from the lane stays in the job
+        const int tid = held(threadIdx.x, turn), lane = tid & 63, w = uniform(tid >> 6), lq = lane & 31, h = lane >> 5;
+        const int row0 = j.grp * RG, rows = min(RG, j.T * p.G - row0), base = j.L - j.T;
+        record_part(p, j, all.jobs, row0, rows);
+        // a chain's later slots are seen by none of the group's rows
+        if (!p.batch.tree) j.k1 = min(j.k1, base + (row0 + rows - 1) / p.G + 1);
 
-    const int my = 32 * w + lq, rr = row0 + min(my, rows - 1), tq = rr / p.G;
-    const size_t tok = size_t(j.first) + tq;
-    s16x8 qf[KS];
-    {
-        const char* qp = p.q + tok * p.q_token + int64_t(j.hk * p.G + rr % p.G) * p.q_head;
+        const int my = 32 * w + lq, rr = row0 + min(my, rows - 1), tq = rr / p.G;
+        const size_t tok = size_t(j.first) + tq;
+        const bool idle = 32 * w >= rows;  // this wave only stages
+        s16x8 qf[KS];
+        {
+            const char* qp = p.q + tok * p.q_token + int64_t(j.hk * p.G + rr % p.G) * p.q_head;
 #pragma unroll
-        for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const s16x8*>(qp + (16 * s + 8 * h) * 2);
-        if (p.scale2 < 0.f) {
-            // the running maximum is one of q.k: the sign of the scale goes to the queries
+            for (int s = 0; s < KS; ++s) qf[s] = *reinterpret_cast<const s16x8*>(qp + (16 * s + 8 * h) * 2);
+            if (p.scale2 < 0.f) {
+                // the running maximum is one of q.k: the sign of the scale goes to the queries
 #pragma unroll
-            for (int s = 0; s < KS; ++s) qf[s] ^= short(0x8000);
+                for (int s = 0; s < KS; ++s) qf[s] ^= short(0x8000);
+            }
         }
-    }
-    const float scale2 = fabsf(p.scale2);
-    const bool idle = 32 * w >= rows;  // this wave only stages
+        settle(qf);
+        const float scale2 = fmaxf(fabsf(p.scale2), 1e-37f);  // not 0, which would make NaN of the masked scores
 
-    f32x16 o[DT];
+        f32x16 o[DT], sc[2];
 #pragma unroll
-    for (int t = 0; t < DT; ++t)
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
-    float m_ref = -__builtin_inff(), l_run = 0.f;
+            for (int i = 0; i < 16; ++i) o[t][i] = 0.f;
+        float m_ref = kLowest, l_run = 0.f;
+        s16x8 pf[2][2] = {};  // weights of the two halves, 16 keys each
 
-    const char* kh = p.pool.k + int64_t(j.hk) * p.pool.k_head;
-    const char* vh = p.pool.v + int64_t(j.hk) * p.pool.v_head;
-    const int32_t* table = p.batch.table + size_t(j.r) * p.batch.width;
-    const int omask = (1 << p.pool.lb) - 1;
+        const char* kh = head_of(p.pool.k, p.pool.k_head, j.hk);
+        const char* vh = head_of(p.pool.v, p.pool.v_head, j.hk);
+        const int32_t* table = p.batch.table + size_t(j.r) * p.batch.width;
+        const int omask = (1 << p.pool.lb) - 1;
 
-    int ids[PIECES], my_id;  // block ids of the staged rows, and of slot k0 + lane
-    const auto load_ids = [&](int k0) {
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const int key = k0 + (tid + NT * i) / CH;
-            ids[i] = key < j.k1 && (EVEN || tid + NT * i < kTile * CH) ? table[key >> p.pool.lb] : -1;
-        }
-        my_id = lane < kTile && k0 + lane < j.k1 ? table[(k0 + lane) >> p.pool.lb] : -1;
-    };
-    s16x8 kr[PIECES], vr[PIECES];
-    uint64_t alive_next = 0;
-    const auto load_tile = [&](int k0) {
-#pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const int key = k0 + (tid + NT * i) / CH, piece = (tid + NT * i) % CH;
-            const bool ok = unsigned(ids[i]) < p.pool.n_blocks;
-            const int64_t blk = ok ? ids[i] : 0, off = ok ? key & omask : 0;
-            kr[i] = *reinterpret_cast<const s16x8*>(kh + blk * p.pool.k_block + off * p.pool.k_token + piece * 16);
-            const s16x8 x = *reinterpret_cast<const s16x8*>(vh + blk * p.pool.v_block + off * p.pool.v_token + piece * 16);
-            vr[i] = ok ? x : s16x8{};
-        }
-        alive_next = __ballot(unsigned(my_id) < p.pool.n_blocks);
-    };
-    // Stores the staged tile; whether values of new tokens were not finite.
-    const auto store_tile = [&](int buf, int k0) {
-        bool odd = false;
-        if (k0 + kTile > base) {
+        // Block ids of a tile, -1 outside the pool and past the end: of the row that this thread stages, and of row `lane`.
+        // The loads are clamped to the job's keys, not branched around.
+        const int my_row = tid / NW, my_piece = (tid % NW) ^ (CH == 2 * NW ? (my_row & 1) * NW : 0);
+        struct Ids {
+            int row, lane;
+        };
+        const auto load_ids = [&](int k0) {
+            const int last = max(j.k1 - 1, 0);
+            return Ids{table[unsigned(min(k0 + my_row, last)) >> p.pool.lb], table[unsigned(min(k0 + lane, last)) >> p.pool.lb]};
+        };
+        const auto valid = [&](int k0, Ids& q) {
+            if (k0 + my_row >= j.k1 || unsigned(q.row) >= p.pool.n_blocks) q.row = -1;
+            return __ballot(k0 + lane < j.k1 && unsigned(q.lane) < p.pool.n_blocks);
+        };
+        const auto piece_of = [&](int i) { return CH == 2 * NW ? my_piece ^ (i * NW) : my_piece + i * NW; };
+        const auto load_rows = [&](const char* head, uint32_t block, uint32_t token, int k0, int id, s16x8 (&x)[PIECES]) {
+            const char* at = row_of(head, block, token, max(id, 0), id < 0 ? 0 : (k0 + my_row) & omask);
 #pragma unroll
             for (int i = 0; i < PIECES; ++i)
+                if (EVEN || piece_of(i) < CH) x[i] = *reinterpret_cast<const s16x8*>(at + piece_of(i) * 16);
+        };
+        const auto store_keys = [&](char* to, const s16x8 (&x)[PIECES]) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const bool bad = (unsigned(vr[i][e]) & T::kExp) == T::kExp;
-                    odd |= bad;
-                    vr[i][e] = bad ? short(0) : vr[i][e];
-                }
-        }
+            for (int i = 0; i < PIECES; ++i)
+                if (EVEN || piece_of(i) < CH) *reinterpret_cast<s16x8*>(to + my_row * D * 2 + ((piece_of(i) ^ swz_rows<D>(my_row)) * 16)) = x[i];
+        };
+        // Unseen slots weigh nothing whatever they hold: what lies outside the pool goes in as zeros, and so do values of new
+        // tokens that are not finite; returns whether there were any.
+        const auto store_values = [&](char* to, s16x8 (&x)[PIECES], int id, bool whole, bool fresh) {
+            bool odd = false;
+            if (!whole && id < 0) {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            const int row = (tid + NT * i) / CH, piece = (tid + NT * i) % CH;
-            const int at = row * D * 2 + ((piece ^ swz<D>(row)) * 16);
-            if (!EVEN && row >= kTile) continue;
-            *reinterpret_cast<s16x8*>(&ks[buf][at]) = kr[i];
-            *reinterpret_cast<s16x8*>(&vs[buf][at]) = vr[i];
-        }
-        return odd;
-    };
-
-    int k0 = j.k0, buf = 0;
-    bool odd = false;
-    uint64_t alive = 0;
-    if (k0 < j.k1) {
-        load_ids(k0);
-        load_tile(k0);
-        load_ids(k0 + kTile);
-        alive = alive_next;
-        odd = store_tile(0, k0);
-    }
-    for (; k0 < j.k1; k0 += kTile, buf ^= 1) {
-        const bool fresh = k0 + kTile > base;
-        if (fresh)
-            odd = __syncthreads_or(odd);
-        else
-            __syncthreads();
-        const bool more = k0 + kTile < j.k1;
-        if (more) {
-            load_tile(k0 + kTile);
-            load_ids(k0 + 2 * kTile);
-        }
-        if (!idle) {
-            f32x16 sc[UT];
-#pragma unroll
-            for (int u = 0; u < UT; ++u) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) sc[u][i] = 0.f;
-                const int row = 32 * u + lq;
-#pragma unroll
-                for (int s = 0; s < KS; ++s) {
-                    const s16x8 kf = *reinterpret_cast<const s16x8*>(&ks[buf][row * D * 2 + (((2 * s + h) ^ swz<D>(row)) * 16)]);
-                    sc[u] = T::mfma32(kf, qf[s], sc[u]);
-                }
+                for (int i = 0; i < PIECES; ++i) x[i] = s16x8{};
             }
-            uint64_t see = alive;
             if (fresh) {
-                // the slots of the tile that this lane's row sees
-                const int rel = k0 - base;
-                if (!p.batch.tree) {
-                    const int most = tq - rel;
-                    see &= most >= 63 ? ~0ull : most < 0 ? 0ull : (2ull << most) - 1;
-                } else {
-                    const uint64_t* bits = p.batch.tree + tok * p.batch.words;
-                    const auto word = [&](int i) { return i >= 0 && i < p.batch.words ? bits[i] : 0ull; };
-                    if (rel >= 0) {
-                        const int i = rel >> 6, s = rel & 63;
-                        see &= (word(i) >> s) | (s ? word(i + 1) << (64 - s) : 0ull);
-                    } else if (rel > -64) {
-                        see &= (word(0) << -rel) | ((1ull << -rel) - 1);
+#pragma unroll
+                for (int i = 0; i < PIECES; ++i)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const bool bad = (EVEN || piece_of(i) < CH) && (unsigned(x[i][e]) & T::kExp) == T::kExp;
+                        odd |= bad;
+                        x[i][e] = bad ? short(0) : x[i][e];
+                    }
+            }
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i)
+                if (EVEN || piece_of(i) < CH) *reinterpret_cast<s16x8*>(to + my_row * D * 2 + ((piece_of(i) ^ swz_tr32<D>(my_row)) * 16)) = x[i];
+            return odd;
+        };
+        int k0 = j.k0;
+        // A lane's pieces differ by an exclusive or (or, where rows of 96 elements keep it apart, a sum) from the first one's
+        // address.  `held` keeps the compiler from having all of them in registers at once.
+        const int key_at = lq * D * 2 + ((h ^ swz_rows<D>(lq)) * 16);
+        const int tr_row = 4 * h + ((lane & 15) >> 2);
+        const int value_at = tr_row * D * 2 + (((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ swz_tr32<D>(tr_row)) * 16) + (lane & 1) * 8;
+        const auto key_piece = [&](const char* keys, auto u, int at, int i) {
+            const int piece = D == 96 ? (at ^ ((i & 1) << 5)) + 64 * (i >> 1) : at ^ (i << 5);
+            return *reinterpret_cast<const s16x8*>(keys + piece + 32 * u * D * 2);
+        };
+        // i: 16 keys and 32 dimensions, dimensions first
+        const auto value_piece = [&](const char* values, auto u, int at, int i) {
+            const int t = i % DT, piece = D == 96 ? at + (t << 6) : at ^ (t << 6);
+            s16x8 a;
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {
+                const s16x4 x4 = read_tr16(values + piece + (32 * u + 16 * (i / DT) + 8 * g) * D * 2);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) a[4 * g + e] = x4[e];
+            }
+            return a;
+        };
+        // Scores of half u of the keys in a buffer, half u of the values in a buffer weighted: the first and the last product.
+        const auto scores = [&](const char* keys, auto u, f32x16& s) {
+            const int at = held(key_at, k0);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = 0.f;
+#pragma unroll
+            for (int i = 0; i < KS; ++i) s = T::mfma32(key_piece(keys, u, at, i), qf[i], s);
+        };
+        const auto weighted = [&](const char* values, auto u) {
+            const int at = held(value_at, k0);
+#pragma unroll
+            for (int i = 0; i < KS; ++i) o[i % DT] = T::mfma32(value_piece(values, u, at, i), pf[u][i / DT], o[i % DT]);
+        };
+        uint64_t see = 0;  // the slots of the present tile that this lane's row sees
+        // Half u of the present tile becomes weights while the next half's scores and the last half's output are multiplied.
+        const auto step = [&](auto u, bool masked, const char* next_keys, const char* last_values) {
+            f32x16& s = sc[u];
+            if (masked) {
+                const unsigned bits = unsigned(see >> (32 * u)) >> (4 * h);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = (bits >> (8 * (i / 4) + i % 4)) & 1 ? s[i] : -__builtin_inff();
+            }
+            // One product, two pieces read for the one after next, a share of the softmax, in turn: the order is fixed here, since
+            // the compiler's own puts the products side by side.
+            constexpr Int<1 - u> other;
+            const int ka = held(key_at, k0), va = held(value_at, k0);
+            s16x8 kf[2], vf[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                kf[i] = key_piece(next_keys, other, ka, i);
+                vf[i] = value_piece(last_values, other, va, i);
+            }
+            f32x16& n = sc[other];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) n[i] = 0.f;
+            float mx = 0.f, mn = 0.f, alpha = 0.f, sum = 0.f;
+            bool grown = false;
+            const auto share = [&](int slot) {
+                constexpr int FIRST = 3, SLOTS = 2 * KS - FIRST;  // of the exponentials
+                if (slot == 0) {
+                    mx = s[0];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+                    mn = other_half(mx);
+                } else if (slot == 2) {
+                    mx = fmaxf(mx, mn) * scale2;
+                    grown = mx > m_ref + kSlack;
+                    mn = grown ? mx : m_ref;
+                    alpha = exp2_fast(m_ref - mn);
+                    m_ref = mn;
+                } else if (slot >= FIRST) {
+                    const int from = 16 * (slot - FIRST) / SLOTS, to = 16 * (slot - FIRST + 1) / SLOTS;
+#pragma unroll
+                    for (int i = from; i < to; ++i) {
+                        s[i] = exp2_fast(__builtin_fmaf(s[i], scale2, -mn));
+                        sum += s[i];
                     }
                 }
+            };
+#pragma unroll
+            for (int i = 0; i < KS; ++i) {
+                n = T::mfma32(kf[i & 1], qf[i], n);
+                if (i + 2 < KS) kf[i & 1] = key_piece(next_keys, other, ka, i + 2);
+                share(2 * i);
+                __builtin_amdgcn_sched_barrier(0);
+                o[i % DT] = T::mfma32(vf[i & 1], pf[other][i / DT], o[i % DT]);
+                if (i + 2 < KS) vf[i & 1] = value_piece(last_values, other, va, i + 2);
+                share(2 * i + 1);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if (fresh || alive != (kTile == 64 ? ~0ull : 0xffffffffull)) {
-                const uint64_t s = see >> (4 * h);
 #pragma unroll
-                for (int u = 0; u < UT; ++u) {
-                    const unsigned bits = unsigned(s >> (32 * u));
+            for (int k = 0; k < 2; ++k) {
+                f32x8 x;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) sc[u][i] = (bits >> (8 * (i / 4) + i % 4)) & 1 ? sc[u][i] : -__builtin_inff();
-                }
+                for (int i = 0; i < 8; ++i) x[i] = s[8 * k + i];
+                pf[u][k] = pack8<T>(x);
             }
-            float mx = sc[0][0];
-#pragma unroll
-            for (int i = 0; i < 16 * UT; ++i) mx = fmaxf(mx, sc[i >> 4][i & 15]);
-            mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale2;
-            if (__any(mx > m_ref + kSlack)) {
-                const float mn = fmaxf(m_ref, mx);
-                const float alpha = mn == -__builtin_inff() ? 1.f : exp2_fast(m_ref - mn);
-                m_ref = mn;
-                l_run *= alpha;
+            settle(pf[u]);  // here, beside the products, and not behind the branch
+            l_run = l_run * alpha + sum;
+            if (__any(grown)) {
 #pragma unroll
                 for (int t = 0; t < DT; ++t) o[t] *= alpha;
             }
-            const float ref = m_ref == -__builtin_inff() ? 0.f : m_ref;
-            float sum = 0.f;
-#pragma unroll
-            for (int u = 0; u < UT; ++u)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    sc[u][i] = exp2_fast(__builtin_fmaf(sc[u][i], scale2, -ref));
-                    sum += sc[u][i];
-                }
-            l_run += sum;
-#pragma unroll
-            for (int kk = 0; kk < kTile / 16; ++kk) {
-                f32x8 x;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) x[i] = sc[kk >> 1][8 * (kk & 1) + i];
-                const s16x8 pf = pack8<T>(x);
-#pragma unroll
-                for (int t = 0; t < DT; ++t) {
-                    s16x8 a;
-#pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const int row = 16 * kk + 8 * u + 4 * h + ((lane & 15) >> 2), piece = 4 * t + 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-                        const s16x4 x4 = read_tr16(&vs[buf][row * D * 2 + ((piece ^ swz<D>(row)) * 16) + (lane & 1) * 8]);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) a[4 * u + i] = x4[i];
-                    }
-                    o[t] = T::mfma32(a, pf, o[t]);
-                }
-            }
-            if (fresh && odd) {
-                for (int key = 0; key < kTile; ++key) {
-                    if (!((alive >> key) & 1)) continue;
-                    const char* vp = vh + int64_t(table[(k0 + key) >> p.pool.lb]) * p.pool.v_block + int64_t((k0 + key) & omask) * p.pool.v_token;
-                    const bool mine = (see >> key) & 1;
-#pragma unroll
-                    for (int t = 0; t < DT; ++t)
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const short x = reinterpret_cast<const short*>(vp)[32 * t + 8 * (i / 4) + 4 * h + i % 4];
-                            if (mine && (unsigned(x) & T::kExp) == T::kExp) o[t][i] += widen<T>(x);
-                        }
-                }
-            }
-        }
-        if (more) {
-            odd = store_tile(buf ^ 1, k0 + kTile);
-            alive = alive_next;
-        }
-    }
+        };
 
-    l_run += __shfl_xor(l_run, 32);
-    const float M = m_ref;
-    if (my < rows) {
+        s16x8 kr[PIECES] = {}, vr[PIECES] = {};
+        // ids of the tile whose values are in registers, of the one whose keys are, and of the one to load next; which of a
+        // tile's rows lie in the pool, of the present tile and the one after
+        Ids idv = load_ids(k0), idk = load_ids(k0 + kTile), idn;
+        uint64_t alive = valid(k0, idv), alive_next;
+        load_rows(kh, p.pool.k_block, p.pool.k_token, k0, idv.row, kr);
+        load_rows(vh, p.pool.v_block, p.pool.v_token, k0, idv.row, vr);
+        idn = load_ids(k0 + 2 * kTile);
+        store_keys(ks[0], kr);
+        // the first round multiplies the values of no tile by weights of zero
+        for (int i = tid; i < kTile * CH; i += NT) *reinterpret_cast<s16x8*>(&vs[1][i * 16]) = s16x8{};
+        alive_next = valid(k0 + kTile, idk);
+        load_rows(kh, p.pool.k_block, p.pool.k_token, k0 + kTile, idk.row, kr);
+        __syncthreads();
+        if (!idle) scores(ks[0], Int<0>(), sc[0]);
+
+        const auto round = [&](auto buf) {
+            const bool fresh = k0 + kTile > base;
+            store_keys(ks[1 - buf], kr);
+            bool odd = store_values(vs[buf], vr, idv.row, !~alive, fresh);
+            const uint64_t alive_then = valid(k0 + 2 * kTile, idn);
+            load_rows(vh, p.pool.v_block, p.pool.v_token, k0 + kTile, idk.row, vr);
+            load_rows(kh, p.pool.k_block, p.pool.k_token, k0 + 2 * kTile, idn.row, kr);
+            idv = idk;
+            idk = idn;
+            idn = load_ids(k0 + 3 * kTile);
+            const bool masked = fresh || ~alive;
+            if (masked) {
+                see = alive;
+                if (fresh) {
+                    see &= seen_slots(p.batch, tok, tq, k0 - base);
+                }
+            }
+            if (!idle) step(Int<0>(), masked, ks[buf], vs[1 - buf]);
+            if (fresh)
+                odd = __syncthreads_or(odd);
+            else
+                __syncthreads();
+            if (!idle) {
+                step(Int<1>(), masked, ks[1 - buf], vs[buf]);
+                if (fresh && odd) {
+                    for (int key = 0; key < kTile; ++key) {
+                        if (!((alive >> key) & 1)) continue;
+                        const char* vp = row_of(vh, p.pool.v_block, p.pool.v_token, table[(k0 + key) >> p.pool.lb], (k0 + key) & omask);
+                        const bool seen = (see >> key) & 1;
+#pragma unroll
+                        for (int t = 0; t < DT; ++t)
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const short x = reinterpret_cast<const short*>(vp)[32 * t + 8 * (i / 4) + 4 * h + i % 4];
+                                if (seen && (unsigned(x) & T::kExp) == T::kExp) o[t][i] += widen<T>(x);
+                            }
+                    }
+                }
+            }
+            alive = alive_next;
+            alive_next = alive_then;
+            k0 += kTile;
+        };
+        int last = 1;  // the buffer of the last tile's values
+        while (k0 < j.k1) {
+            round(Int<0>());
+            last = 0;
+            if (k0 >= j.k1) break;
+            round(Int<1>());
+            last = 1;
+        }
+        if (!idle) weighted(vs[last], Int<1>());
+
+        l_run += other_half(l_run);
+        if (my >= rows) continue;
         if (j.nsplit == 1) {
             const float inv = l_run > 0.f ? 1.f / l_run : (l_run == 0.f ? 0.f : l_run);
             char* op = p.out + tok * p.out_token + int64_t(j.hk * p.G + rr % p.G) * p.out_head;
@@ -579,7 +648,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void k_attend_tiles(cons
                     const f32x4 x = {o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
                     *reinterpret_cast<s16x4*>(op + 2 * (32 * t + 8 * i + 4 * h)) = pack4<T>(x * inv);
                 }
-            if (h == 0 && p.lse) p.lse[tok * p.q_heads + j.hk * p.G + rr % p.G] = l_run == 0.f ? -__builtin_inff() : M * kLn2 + __logf(l_run);
+            if (h == 0 && p.lse) p.lse[tok * p.q_heads + j.hk * p.G + rr % p.G] = l_run == 0.f ? -__builtin_inff() : m_ref * kLn2 + __logf(l_run);
         } else {
             const size_t at = size_t(j.id) * RG + my;
 #pragma unroll
@@ -588,52 +657,62 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void k_attend_tiles(cons
                 for (int i = 0; i < 4; ++i)
                     *reinterpret_cast<f32x4*>(&p.part_o[at * D + 32 * t + 8 * i + 4 * h]) = f32x4{o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
             if (h == 0) {
-                p.part_ml[2 * at] = M;
+                p.part_ml[2 * at] = m_ref;
                 p.part_ml[2 * at + 1] = l_run;
             }
         }
     }
-    if (j.nsplit > 1) join_splits<T, D, NT>(p, j, row0, rows, RG, &last);
 }
 
-constexpr uint32_t kTarget = 512;
-
+// Rows of a job and the kernel they go to.  Up to 16 rows are a stream over
+// the keys.  More take shared tiles, with four waves where that holds a
+// request's rows in one or two jobs (trees of up to 48 tokens and 5 heads: 265
+// us with 4 waves, 299 us with 8), else with eight, which read the keys half as
+// often (chunks of 2048 tokens and 4 heads: 767 us with 8, 857 us with 4).
+// Rows of 256 elements leave room for four waves only.
+//
+// Jobs to aim for: two a compute unit for the stream (a decode of 150 requests
+// takes 122, 100, 105, 111 us at 256, 512, 1024, 2048), one for the tiles (265
+// us the trees, 284 us at 512), whose parts are large.
 struct Sizes {
-    uint32_t rows;  // query rows of a job
+    uint32_t rows;    // query rows of a job
+    uint32_t target;  // jobs to aim for
     uint64_t jobs;
-    size_t ml, o;   // bytes of the two partial arrays
-    size_t total;
+    size_t part, ml, o, total;  // byte offsets in the workspace and its size
 };
-
-// The counters of the splits take the first 64th of the workspace, whatever a
-// call's sizes, so that no call's partial rows lie where a later one counts.
-// A job's rows are at least 16 (8 + 256) bytes: its 4-byte counter always fits.
-constexpr size_t kCountShare = 64;
-static size_t count_bytes(size_t workspace) { return workspace / kCountShare & ~size_t(255); }
 
 static Sizes sizes(uint32_t n, uint32_t n_tokens, uint32_t max_q, uint32_t q_heads, uint32_t kv_heads, uint32_t head_dim)
 {
     const uint32_t G = q_heads / kv_heads;
     Sizes s;
     const uint64_t most = uint64_t(max_q) * G;
-    s.rows = most <= 16 ? 16 : most <= 128 || head_dim == 256 ? 128 : 256;
-    s.jobs = max_jobs(n, n_tokens, kv_heads, G, s.rows, kTarget);
-    s.ml = align256(8 * s.jobs * s.rows);
-    s.o = align256(4 * s.jobs * s.rows * head_dim);
-    s.total = align256((s.ml + s.o) / (kCountShare - 1) * kCountShare + 2 * 256 * kCountShare);
+    s.rows = most <= 16 ? 16 : most <= 256 || head_dim == 256 ? 128 : 256;
+    s.target = s.rows == 16 ? 512 : 256;
+    s.jobs = max_jobs(n, n_tokens, kv_heads, G, s.rows, s.target);
+    s.part = 256;
+    s.ml = s.part + align256(sizeof(Part) * s.jobs);
+    s.o = s.ml + align256(8 * s.jobs * s.rows);
+    s.total = s.o + align256(4 * s.jobs * s.rows * head_dim);
     return s;
+}
+
+template <class K>
+static void launch_jobs(K kernel, int threads, const AttendP& p, const Sizes& s, hipStream_t stream)
+{
+    static const uint32_t at_once = held_at_once(reinterpret_cast<const void*>(kernel), threads);
+    hipLaunchKernelGGL(kernel, dim3(launch_groups(s.jobs, at_once)), dim3(threads), 0, stream, p);
 }
 
 template <class T, int D>
 static void launch_d(const AttendP& p, const Sizes& s, hipStream_t stream)
 {
-    const dim3 grid(uint32_t(s.jobs));
     if (s.rows == 16)
-        hipLaunchKernelGGL((k_attend_rows<T, D, 1>), grid, dim3(256), 0, stream, p);
+        launch_jobs(k_attend_rows<T, D, 1>, 256, p, s, stream);
     else if (s.rows == 128)
-        hipLaunchKernelGGL((k_attend_tiles<T, D, 4>), grid, dim3(256), 0, stream, p);
+        launch_jobs(k_attend_tiles<T, D, 4>, 256, p, s, stream);
     else if constexpr (D < 256)
-        hipLaunchKernelGGL((k_attend_tiles<T, D, 8>), grid, dim3(512), 0, stream, p);
+        launch_jobs(k_attend_tiles<T, D, 8>, 512, p, s, stream);
+    hipLaunchKernelGGL((k_attend_join<T, D>), dim3(uint32_t(s.jobs), s.rows == 16 ? 1 : 4), dim3(256), 0, stream, p, int(s.rows));
 }
 
 template <class T>
@@ -692,11 +771,11 @@ int mts_attend(const mts_attend_args* a, hipStream_t stream)
     p.q_heads = int(a->q_heads);
     p.G = int(a->q_heads / a->pool.kv_heads);
     p.scale2 = a->scale * kLog2e;
-    p.count = reinterpret_cast<unsigned*>(ws);
-    ws += count_bytes(a->workspace_bytes);
-    p.part_ml = reinterpret_cast<float*>(ws);
-    p.part_o = reinterpret_cast<float*>(ws + s.ml);
-    p.target = int(kTarget);
+    p.jobs = reinterpret_cast<int*>(ws);
+    p.part = reinterpret_cast<Part*>(ws + s.part);
+    p.part_ml = reinterpret_cast<float*>(ws + s.ml);
+    p.part_o = reinterpret_cast<float*>(ws + s.o);
+    p.target = int(s.target);
     if (a->pool.type == MTS_BF16)
         launch_t<Bf16>(p, a->pool.head_dim, s, stream);
     else

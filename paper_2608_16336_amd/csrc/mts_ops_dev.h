@@ -85,6 +85,39 @@ __device__ __forceinline__ void lds_order()
     __builtin_amdgcn_wave_barrier();
 }
 
+// The value of the lane 32 lanes away.
+__device__ __forceinline__ float other_half(float x)
+{
+    const unsigned u = __float_as_uint(x);
+    const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);  // the lower half's values twice, the upper half's twice
+    return __uint_as_float(__lane_id() < 32 ? s[1] : s[0]);
+}
+
+// x, as if it depended on `turn`: what is computed from it stays in the loop
+// that changes `turn`, instead of in registers throughout.
+__device__ __forceinline__ int held(int x, int turn)
+{
+    asm("" : "+v"(x) : "s"(turn));
+    return x;
+}
+
+// Has the loads of these registers waited for here.  Registers that a loop
+// reads without writing would else be waited for inside it, and with them the
+// younger loads that the loop has on their way.
+template <int N>
+__device__ __forceinline__ void settle(s16x8 (&x)[N])
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
+}
+
+// A KV head's part of a pool, and in it the row of a block's token.  Offsets take 64 bits.
+__device__ __forceinline__ const char* head_of(const char* pool, uint32_t head, int hk) { return pool + (uint64_t(head) * unsigned(hk) << 4); }
+__device__ __forceinline__ const char* row_of(const char* head, uint32_t block, uint32_t token, int blk, int off)
+{
+    return head + ((uint64_t(block) * unsigned(blk) + uint64_t(token) * unsigned(off)) << 4);
+}
+
 __device__ __forceinline__ int request_len(const Pool& p, const Batch& b, int r)
 {
     const int most = b.width << p.lb;
@@ -101,10 +134,50 @@ __device__ __forceinline__ void request_tokens(const Batch& b, int r, int& first
     T = z - a < b.max_q ? z - a : b.max_q;
 }
 
+// Staged rows lie row after row, their 16-byte pieces swapped by row so that
+// one instruction's reads fall on different banks (64 of 4 bytes): rows of 128
+// and 256 elements start on the same bank, those of 64 on one of two, those of
+// 96 on one of four.  Swapped are the pieces' numbers, by exclusive or.
+//   swz_rows: 16 bytes of each of 16 rows
+//   swz_tr32: 64 bytes of each of 4 rows (a half wave's transposed read)
+//   swz_tr16: 32 bytes of each of 8 rows
+template <int D>
+__device__ __forceinline__ int swz_rows(int row)
+{
+    return D == 64 ? (row >> 1) & 7 : D == 96 ? (row >> 2) & 3 : row & 15;
+}
+template <int D>
+__device__ __forceinline__ int swz_tr32(int row)
+{
+    return D == 64 ? ((row >> 1) & 1) << 2 : D == 96 ? 0 : (row & 3) << 2;
+}
+template <int D>
+__device__ __forceinline__ int swz_tr16(int row)
+{
+    return D == 64 ? ((row >> 1) & 3) << 1 : D == 96 ? ((row >> 2) & 1) << 1 : (row & 7) << 1;
+}
+
+// Which of the 64 slots from offset rel among the new ones on (negative: before them) new token t, the call's token
+// `tok`, may see.
+__device__ __forceinline__ uint64_t seen_slots(const Batch& b, size_t tok, int t, int rel)
+{
+    if (!b.tree) {
+        const int most = t - rel;
+        return most >= 63 ? ~0ull : most < 0 ? 0ull : (2ull << most) - 1;
+    }
+    const uint64_t* bits = b.tree + tok * b.words;
+    const auto word = [&](int i) { return i >= 0 && i < b.words ? bits[i] : 0ull; };
+    if (rel >= 0) {
+        const int i = rel >> 6, s = rel & 63;
+        return (word(i) >> s) | (s ? word(i + 1) << (64 - s) : 0ull);
+    }
+    return rel > -64 ? (word(0) << -rel) | ((1ull << -rel) - 1) : ~0ull;
+}
+
 // One job: part `split` of `nsplit` of request r's keys [k0, k1), for KV head
-// hk and one group of its query rows.  `lead` is the id of the split 0 job.
+// hk and one group of its query rows; the job of the next split is id + step.
 struct Job {
-    int id, lead;
+    int id, step;
     int r, hk, grp, split, nsplit;
     int L, T, first;
     int k0, k1;
@@ -115,30 +188,29 @@ struct SplitRule {
     int rows;         // query rows (token x head of the group) of a job; 0: all
     int G;            // query heads a KV head
     int target;       // jobs to aim for
-    bool xcd;         // neighbouring jobs (which share keys) to one of the 8 dies
 };
 
 template <int NW>
 __device__ __forceinline__ int64_t block_sum(int64_t v, int64_t* scratch)
 {
     for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    __syncthreads();
     if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
     __syncthreads();
     int64_t s = 0;
 #pragma unroll
     for (int i = 0; i < NW; ++i) s += scratch[i];
-    __syncthreads();
     return s;
 }
 
 // What one request adds: groups of query rows, rounds over its keys.
 struct Share {
-    int L, T, first, groups, rounds;
+    int r, L, T, first, groups, rounds;
 };
 
 __device__ __forceinline__ Share share_of(const Pool& p, const Batch& b, const SplitRule& s, int r)
 {
-    Share q{0, 0, 0, 0, 1};
+    Share q{r, 0, 0, 0, 0, 1};
     if (r < b.n) {
         q.L = request_len(p, b, r);
         request_tokens(b, r, q.first, q.T);
@@ -148,90 +220,155 @@ __device__ __forceinline__ Share share_of(const Pool& p, const Batch& b, const S
     return q;
 }
 
-// The jobs of a ragged batch, numbered head by head, in it request by request,
-// group by group, split by split.  Lengths live on the device, so every
-// workgroup (NW waves) finds its own job: it sums the requests' rounds, takes
-// as many rounds a job as leave about `target` jobs, and finds its number
-// among the requests' job counts.  One request a thread; more are passed over
-// in turns.  Returns false for numbers past the last job; the results are
-// uniform.  scratch: NW + 4 words of LDS.
-template <int NW>
-__device__ __forceinline__ bool find_job(const Pool& p, const Batch& b, const SplitRule& s, Job& j, int64_t* scratch)
+// A value that all lanes have alike, in a scalar register.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x)
 {
-    constexpr int NT = 64 * NW;
-    const int t = threadIdx.x;
-    Share q{};
-    int64_t rounds = 0;
-    for (int r0 = 0; r0 < b.n; r0 += NT) {
-        q = share_of(p, b, s, r0 + t);
-        rounds += int64_t(q.rounds) * q.groups;
+    return int64_t(uint64_t(unsigned(uniform(int(uint64_t(x) >> 32)))) << 32 | unsigned(uniform(int(x))));
+}
+
+// The jobs of a ragged batch.  Lengths live on the device, so every workgroup
+// (NW waves) of a launch finds out for itself what there is to do: it sums the
+// requests' rounds and takes as many rounds a job as leave about `target`
+// jobs.  Jobs are numbered head by head, in it request by request, longest
+// first (as far as there is one a thread; more are passed over in turns), in
+// it split by split and group by group.
+//
+// A workgroup takes several jobs: the launch has as many workgroups as the
+// chip holds at once, because one a job, given out by the hardware in turns,
+// left compute units idle (a fifth of the time of equal chunks of prompts).
+// Each of the 8 dies (workgroups go to them in turn) has an eighth of the
+// numbers, so that jobs of a head, which share keys, share a cache; in it the
+// workgroups count forth and back, so that who began with a long job ends with
+// a short one.
+template <int NW>
+struct Jobs {
+    static constexpr int NT = 64 * NW;
+    const Pool& p;
+    const Batch& b;
+    const SplitRule& s;
+    int64_t* scratch;  // NW + 4 words of LDS
+    int* order;        // [NT] the thread's request, and how many of a head's jobs come before it: in LDS, not in registers
+    int64_t* before;   // [NT]
+    int per;
+    int64_t head, jobs;  // jobs of a head, of all
+
+    __device__ __forceinline__ int64_t count(const Share& x) const { return int64_t((x.rounds + per - 1) / per) * x.groups; }
+
+    __device__ __forceinline__ Jobs(const Pool& p_, const Batch& b_, const SplitRule& s_, int64_t* scratch_) : p(p_), b(b_), s(s_), scratch(scratch_)
+    {
+        __shared__ int order_[NT];
+        __shared__ int64_t before_[NT];
+        order = order_;
+        before = before_;
+        const int t = threadIdx.x;
+        Share q{};
+        int64_t rounds = 0;
+        for (int r0 = 0; r0 < b.n; r0 += NT) {
+            q = share_of(p, b, s, r0 + t);
+            rounds += int64_t(q.rounds) * q.groups;
+        }
+        const int64_t total = block_sum<NW>(rounds, scratch) * p.kv_heads;
+        per = uniform(total > s.target ? int((total + s.target - 1) / s.target) : 1);
+        if (b.n <= NT) {
+            int* len = reinterpret_cast<int*>(before);
+            len[t] = q.rounds;
+            __syncthreads();
+            if (t < b.n) {
+                int rank = 0;
+                for (int i = 0; i < b.n; ++i) rank += len[i] > q.rounds || (len[i] == q.rounds && i < t);
+                order[rank] = t;
+            }
+            __syncthreads();
+            if (t < b.n) q = share_of(p, b, s, order[t]);
+            head = uniform(prefix(count(q), 0));
+        } else {
+            int64_t n = 0;
+            for (int r0 = 0; r0 < b.n; r0 += NT) n += count(share_of(p, b, s, r0 + t));
+            head = uniform(block_sum<NW>(n, scratch));
+        }
+        jobs = head * p.kv_heads;
     }
-    const int64_t total = block_sum<NW>(rounds, scratch) * p.kv_heads;
-    const int per = total > s.target ? int((total + s.target - 1) / s.target) : 1;
-    int64_t mine = 0;
-    for (int r0 = 0; r0 < b.n; r0 += NT) {
-        if (b.n > NT) q = share_of(p, b, s, r0 + t);
-        mine += int64_t((q.rounds + per - 1) / per) * q.groups;
-    }
-    const int64_t head = block_sum<NW>(mine, scratch), jobs = head * p.kv_heads;
-    int64_t id = blockIdx.x;
-    if (s.xcd) {
-        const int64_t chunk = (jobs + 7) / 8;
-        if ((id >> 3) >= chunk) return false;
-        id = (id & 7) * chunk + (id >> 3);
-    }
-    if (id >= jobs) return false;
-    const int hk = int(id / head), in = int(id % head);
-    int* found = reinterpret_cast<int*>(scratch + NW);
-    int64_t before = 0;
-    for (int r0 = 0; r0 < b.n; r0 += NT) {
-        if (b.n > NT) q = share_of(p, b, s, r0 + t);
-        const int ns = (q.rounds + per - 1) / per;
-        const int64_t n = int64_t(ns) * q.groups;
+
+    // before[] of one request a thread, from n of each and `from` before them; returns what comes after them
+    __device__ __forceinline__ int64_t prefix(int64_t n, int64_t from)
+    {
+        const int t = threadIdx.x;
         int64_t incl = n;
         for (int o = 1; o < 64; o <<= 1) {
             const int64_t v = __shfl_up(incl, o);
             if ((t & 63) >= o) incl += v;
         }
-        if ((t & 63) == 63) scratch[t >> 6] = incl;
-        if (t == 0) found[0] = -1;
         __syncthreads();
-        int64_t base = before;
+        if ((t & 63) == 63) scratch[t >> 6] = incl;
+        __syncthreads();
+        int64_t all = 0;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            if (w < (t >> 6)) base += scratch[w];
-            before += scratch[w];
+            if (w < (t >> 6)) from += scratch[w];
+            all += scratch[w];
         }
-        const int64_t at = in - (base + incl - n);
-        if (at >= 0 && at < n) {
-            found[0] = r0 + t;
-            found[1] = int(at);
-            found[2] = ns;
-            found[3] = q.L;
-            found[4] = q.T;
-            found[5] = q.first;
-        }
+        before[t] = from + incl - n;
         __syncthreads();
-        if (found[0] >= 0) break;
+        return before[0] + all;
     }
-    const int at = __builtin_amdgcn_readfirstlane(found[1]);
-    j.id = int(id);
-    j.hk = hk;
-    j.r = __builtin_amdgcn_readfirstlane(found[0]);
-    j.nsplit = __builtin_amdgcn_readfirstlane(found[2]);
-    j.L = __builtin_amdgcn_readfirstlane(found[3]);
-    j.T = __builtin_amdgcn_readfirstlane(found[4]);
-    j.first = __builtin_amdgcn_readfirstlane(found[5]);
-    j.split = at % j.nsplit;
-    j.grp = at / j.nsplit;
-    j.lead = j.id - j.split;
-    const int64_t k0 = int64_t(j.split) * per * s.unit, k1 = k0 + int64_t(per) * s.unit;
-    j.k0 = int(k0);
-    j.k1 = int(k1 < j.L ? k1 : j.L);
-    return true;
+
+    // The turn-th job of this workgroup; false past the last one.  Uniform, with barriers.
+    __device__ __forceinline__ bool get(int turn, Job& j)
+    {
+        const int64_t chunk = (jobs + 7) / 8, wide = gridDim.x >> 3, at = blockIdx.x >> 3;
+        const int64_t local = turn * wide + (turn & 1 ? wide - 1 - at : at), id = (blockIdx.x & 7) * chunk + local;
+        if (local >= chunk || id >= jobs) return false;
+        const int t = threadIdx.x, hk = int(id / head);
+        const int64_t in = id % head;
+        int* found = reinterpret_cast<int*>(scratch + NW);
+        __syncthreads();
+        int64_t end = head;  // of the requests in before[]
+        int64_t from = 0;
+        for (int r0 = 0; r0 < b.n; r0 += NT) {
+            if (b.n > NT) from = end = prefix(count(share_of(p, b, s, r0 + t)), from);
+            // requests without jobs have the next one's number: the last of equal ones has them
+            const int last = b.n - r0 < NT ? b.n - r0 : NT;
+            if (t < last && before[t] <= in && in < (t + 1 < last ? before[t + 1] : end)) {
+                found[0] = b.n > NT ? r0 + t : order[t];
+                found[1] = int(in - before[t]);
+            }
+            __syncthreads();
+            if (in < end) break;
+        }
+        const Share q = share_of(p, b, s, uniform(found[0]));
+        const int i = uniform(found[1]), rounds = uniform(q.rounds);
+        j.id = int(id);
+        j.hk = hk;
+        j.r = q.r;
+        j.step = uniform(q.groups);
+        j.L = uniform(q.L);
+        j.T = uniform(q.T);
+        j.first = uniform(q.first);
+        j.nsplit = (rounds + per - 1) / per;
+        j.split = i / j.step;
+        j.grp = i % j.step;
+        const int64_t k0 = int64_t(j.split) * per * s.unit, k1 = k0 + int64_t(per) * s.unit;
+        j.k0 = int(k0);
+        j.k1 = int(k1 < j.L ? k1 : j.L);
+        return true;
+    }
+};
+
+// Workgroups of a launch: a multiple of the 8 dies, no more than there are jobs.
+inline uint32_t launch_groups(uint64_t most_jobs, uint32_t at_once) { return uint32_t(((most_jobs < at_once ? most_jobs : at_once) + 7) / 8 * 8); }
+// How many workgroups of a kernel the chip's 256 compute units hold at once.
+inline uint32_t held_at_once(const void* kernel, int threads)
+{
+    int n = 0;
+    if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, 0) != hipSuccess || n < 1) {
+        (void)hipGetLastError();
+        n = 1;
+    }
+    return 256u * uint32_t(n);
 }
 
-// Most jobs that find_job can number for a call of these sizes.
+// Most jobs that there can be for a call of these sizes.
 inline uint64_t max_jobs(uint32_t n, uint64_t n_tokens, uint32_t kv_heads, uint32_t G, uint32_t rows, uint32_t target)
 {
     const uint64_t groups = rows ? n + n_tokens * G / rows : n;

@@ -18,107 +18,106 @@ struct WeighP {
 
 constexpr int kWeighRound = 128;  // keys of one round of a workgroup: 4 waves x 32
 
-// Every key's weight is one job's alone, so nothing is joined: a wave holds 32
-// keys in the matrix instruction's layout and passes over the query rows, 16
-// at a time; a lane's scores S^T = K Q^T are 8 keys of one query, so weights
-// add up in the lane and over the 16 lanes of a group at the end.
+// A key's weight is one job's alone, so nothing is joined.  A wave holds 32
+// keys, straight from memory in the matrix instruction's layout, and passes
+// over the query rows, 32 at a time, which lie in LDS (all of a request's, or
+// ROWS of them in turn where there are more).  A lane's scores S^T = K Q^T are
+// 16 keys of one query: weights add up in the lane, and over the 32 lanes at
+// the end, where each step of the exchange halves what a lane still holds.
 template <class T, int D>
-__global__ __launch_bounds__(256, 2) void k_weigh(const WeighP p)
+__global__ __launch_bounds__(256, D == 256 ? 2 : 4) void k_weigh(const WeighP p)
 {
-    constexpr int KS = D / 32;
+    constexpr int KS = D / 16, CH = D / 8, ROWS = D == 256 ? 64 : 128;
+    __shared__ __attribute__((aligned(16))) char qs[ROWS * D * 2];
+    __shared__ float refs[ROWS];
     __shared__ int64_t scratch[8];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, lq = lane & 15, c = lane >> 4;
-    Job j;
-    const SplitRule rule{kWeighRound, 0, p.G, p.target, false};
-    if (!find_job<4>(p.pool, p.batch, rule, j, scratch)) return;
-    const int rows = j.T * p.G, base = j.L - j.T;
-    const char* kh = p.pool.k + int64_t(j.hk) * p.pool.k_head;
+    const SplitRule rule{kWeighRound, 0, p.G, p.target};
+    Jobs<4> all(p.pool, p.batch, rule, scratch);
     const int omask = (1 << p.pool.lb) - 1;
-    // the next tile's keys are on their way during the present one's rows, their block ids a tile earlier still
-    int ids[2], held[2];
-    s16x8 kn[2][KS];
-    const auto load_ids = [&](int k0) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const int key = k0 + 16 * u + lq;
-            ids[u] = key < j.k1 ? p.batch.table[size_t(j.r) * p.batch.width + (key >> p.pool.lb)] : -1;
-        }
-    };
-    const auto load_tile = [&](int k0) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            const bool ok = unsigned(ids[u]) < p.pool.n_blocks;
-            held[u] = ok ? ids[u] : -1;
-            const char* kp = kh + int64_t(ok ? ids[u] : 0) * p.pool.k_block + int64_t(ok ? (k0 + 16 * u + lq) & omask : 0) * p.pool.k_token;
-#pragma unroll
-            for (int s = 0; s < KS; ++s) kn[u][s] = *reinterpret_cast<const s16x8*>(kp + (32 * s + 8 * c) * 2);
-        }
-    };
-    int k0 = j.k0 + 32 * w;
-    if (k0 < j.k1) {
-        load_ids(k0);
-        load_tile(k0);
-        load_ids(k0 + kWeighRound);
-    }
-    for (; k0 < j.k1; k0 += kWeighRound) {
-        s16x8 kf[2][KS];
-        int id[2];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) {
-            id[u] = held[u];
-#pragma unroll
-            for (int s = 0; s < KS; ++s) kf[u][s] = kn[u][s];
-        }
-        if (k0 + kWeighRound < j.k1) {
-            load_tile(k0 + kWeighRound);
-            load_ids(k0 + 2 * kWeighRound);
-        }
-        float acc[8] = {};
-        const bool fresh = k0 + 32 > base;
-        for (int row0 = 0; row0 < rows; row0 += 16) {
-            const int row = row0 + lq;
-            const bool ok = row < rows;
-            const int t = (ok ? row : 0) / p.G, h = j.hk * p.G + (ok ? row : 0) % p.G;
-            const size_t tok = size_t(j.first) + t;
-            const char* qp = p.q + tok * p.q_token + int64_t(h) * p.q_head;
-            // rows past the end and rows that saw nothing weigh 2^-inf
-            float ref = p.lse[tok * p.q_heads + h] * kLog2e;
-            if (!ok || ref == -__builtin_inff()) ref = __builtin_inff();
-            f32x4 sc[2] = {};
-#pragma unroll
-            for (int s = 0; s < KS; ++s) {
-                const s16x8 qf = *reinterpret_cast<const s16x8*>(qp + (32 * s + 8 * c) * 2);
-                sc[0] = T::mfma16(kf[0][s], qf, sc[0]);
-                sc[1] = T::mfma16(kf[1][s], qf, sc[1]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float x = sc[i >> 2][i & 3] * p.scale2 - ref;
-                bool see = ref != __builtin_inff();
-                if (fresh) {
-                    const int rel = k0 + 16 * (i >> 2) + 4 * c + (i & 3) - base;
-                    if (rel >= 0)
-                        see = see && (p.batch.tree ? rel < 64 * p.batch.words && ((p.batch.tree[tok * p.batch.words + (rel >> 6)] >> (rel & 63)) & 1)
-                                                   : rel <= t);
+    Job j;
+    for (int turn = 0; all.get(turn, j); ++turn) {
+        // held: what follows from the lane stays in the job
+        const int tid = held(threadIdx.x, turn), lane = tid & 63, w = uniform(tid >> 6), lq = lane & 31, h = lane >> 5;
+        const int rows = j.T * p.G, base = j.L - j.T;
+        const char* kh = head_of(p.pool.k, p.pool.k_head, j.hk);
+        // rows [row0, row0 + ROWS) and their lse in powers of two; rows past the end and rows that saw nothing get +inf
+        const auto stage = [&](int row0) {
+            __syncthreads();
+            for (int i = tid; i < ROWS * CH; i += 256) {
+                const int row = i / CH, piece = i % CH, at = row0 + row;
+                if (row0 + (row & ~31) >= rows) break;
+                const int t = (at < rows ? at : 0) / p.G, g = (at < rows ? at : 0) % p.G;
+                const size_t tok = size_t(j.first) + t;
+                s16x8 x = {};
+                if (at < rows) x = *reinterpret_cast<const s16x8*>(p.q + tok * p.q_token + int64_t(j.hk * p.G + g) * p.q_head + piece * 16);
+                *reinterpret_cast<s16x8*>(&qs[row * D * 2 + ((piece ^ swz_rows<D>(row)) * 16)]) = x;
+                if (piece == 0) {
+                    const float ref = p.lse[tok * p.q_heads + j.hk * p.G + g] * kLog2e;
+                    refs[row] = at < rows && ref != -__builtin_inff() ? ref : __builtin_inff();
                 }
-                acc[i] += see ? exp2_fast(x) : 0.f;
             }
-        }
+            __syncthreads();
+        };
+        if (rows <= ROWS) stage(0);
+        // block ids are read a tile ahead of its keys
+        int next;
+        const auto load_id = [&](int k0) { next = k0 + lq < j.k1 ? p.batch.table[size_t(j.r) * p.batch.width + ((k0 + lq) >> p.pool.lb)] : -1; };
+        load_id(j.k0 + 32 * w);
+        for (int kr = j.k0; kr < j.k1; kr += kWeighRound) {
+            const int k0 = kr + 32 * w;
+            const int id = unsigned(next) < p.pool.n_blocks ? next : -1;
+            s16x8 kf[KS];
+            const char* kp = row_of(kh, p.pool.k_block, p.pool.k_token, max(id, 0), id < 0 ? 0 : (k0 + lq) & omask);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+            for (int s = 0; s < KS; ++s) kf[s] = *reinterpret_cast<const s16x8*>(kp + (2 * s + h) * 16);
+            load_id(k0 + kWeighRound);
+            float acc[16] = {};
+            const bool fresh = k0 + 32 > base;
+            for (int row0 = 0; row0 < rows; row0 += ROWS) {
+                if (rows > ROWS) stage(row0);
+                for (int r = 0; r < ROWS && row0 + r < rows; r += 32) {
+                    const float ref = refs[r + lq];
+                    f32x16 sc;
 #pragma unroll
-            for (int o = 1; o < 16; o <<= 1) acc[i] += __shfl_xor(acc[i], o);
-        // lane lq < 8 of a group writes its 4c + lq % 4 of half lq / 4
-        float mine = acc[0];
+                    for (int i = 0; i < 16; ++i) sc[i] = 0.f;
+                    const int at = held((r + lq) * D * 2 + ((h ^ swz_rows<D>(r + lq)) * 16), r);
 #pragma unroll
-        for (int i = 1; i < 8; ++i) mine = lq == i ? acc[i] : mine;
-        const int in = 16 * (lq >> 2) + 4 * c + (lq & 3), key = k0 + in;
-        // the block of that key is known to the lane that loaded it
-        const int b0 = __shfl(id[0], in & 15), b1 = __shfl(id[1], in & 15);
-        const int b = in < 16 ? b0 : b1;
-        if (lq < 8 && b >= 0) {
-            float* at = p.score + ((size_t(b) * p.pool.kv_heads + j.hk) << p.pool.lb) + (key & omask);
-            *at = p.decay == 0.f || key >= base ? mine : p.decay * *at + mine;
+                    for (int s = 0; s < KS; ++s) {
+                        const int piece = D == 96 ? (at ^ ((s & 1) << 5)) + 64 * (s >> 1) : at ^ (s << 5);
+                        sc = T::mfma32(kf[s], *reinterpret_cast<const s16x8*>(qs + piece), sc);
+                    }
+                    if (fresh || __any(ref == __builtin_inff())) {
+                        // a row counts where it sees the slot, whatever unseen slots hold
+                        const int at_row = min(row0 + r + lq, rows - 1), t = at_row / p.G;
+                        const uint64_t see = ref == __builtin_inff() ? 0ull : fresh ? seen_slots(p.batch, size_t(j.first) + t, t, k0 - base) : ~0ull;
+                        const unsigned bits = unsigned(see) >> (4 * h);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            acc[i] += (bits >> (8 * (i / 4) + i % 4)) & 1 ? exp2_fast(__builtin_fmaf(sc[i], p.scale2, -ref)) : 0.f;
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[i] += exp2_fast(__builtin_fmaf(sc[i], p.scale2, -ref));
+                    }
+                }
+            }
+            // bit 4 of the lane's number keeps the upper or lower eight sums, bit 3 of these the upper or lower four, ...
+            int key = k0 + 4 * h;
+#pragma unroll
+            for (int o = 16, n = 8; n; o >>= 1, n >>= 1) {
+                const bool up = lane & o;
+#pragma unroll
+                for (int i = 0; i < n; ++i) {
+                    const float keep = up ? acc[n + i] : acc[i], give = up ? acc[i] : acc[n + i];
+                    acc[i] = keep + __shfl_xor(give, o);
+                }
+                key += up ? (n >= 4 ? 2 * n : n) : 0;  // sums 8 and 4 stand for keys 16 and 8, sums 2 and 1 for keys 2 and 1
+            }
+            const float mine = acc[0] + __shfl_xor(acc[0], 1);
+            const int block = __shfl(id, (key - k0) & 31);  // the lane that loaded the key knows its block
+            if (!(lane & 1) && block >= 0) {
+                float* at = p.score + ((size_t(block) * p.pool.kv_heads + j.hk) << p.pool.lb) + (key & omask);
+                *at = p.decay == 0.f || key >= base ? mine : p.decay * *at + mine;
+            }
         }
     }
 }
@@ -318,13 +317,13 @@ __global__ __launch_bounds__(256) void k_evict_move(const EvictP p, const int pi
         const int a = src[m], b = dst[m];
         const int ia = table[a >> p.pool.lb], ib = table[b >> p.pool.lb];
         if (unsigned(ia) >= p.pool.n_blocks || unsigned(ib) >= p.pool.n_blocks) continue;
-        const int64_t oa = a & omask, ob = b & omask;
-        const int64_t ka = ia * p.pool.k_block + hk * p.pool.k_head + oa * p.pool.k_token + d;
-        const int64_t kb = ib * p.pool.k_block + hk * p.pool.k_head + ob * p.pool.k_token + d;
-        const int64_t va = ia * p.pool.v_block + hk * p.pool.v_head + oa * p.pool.v_token + d;
-        const int64_t vb = ib * p.pool.v_block + hk * p.pool.v_head + ob * p.pool.v_token + d;
-        *reinterpret_cast<u32x4*>(const_cast<char*>(p.pool.k) + kb) = *reinterpret_cast<const u32x4*>(p.pool.k + ka);
-        *reinterpret_cast<u32x4*>(const_cast<char*>(p.pool.v) + vb) = *reinterpret_cast<const u32x4*>(p.pool.v + va);
+        const int oa = a & omask, ob = b & omask;
+        const char* kh = head_of(p.pool.k, p.pool.k_head, hk);
+        const char* vh = head_of(p.pool.v, p.pool.v_head, hk);
+        *reinterpret_cast<u32x4*>(const_cast<char*>(row_of(kh, p.pool.k_block, p.pool.k_token, ib, ob)) + d) =
+            *reinterpret_cast<const u32x4*>(row_of(kh, p.pool.k_block, p.pool.k_token, ia, oa) + d);
+        *reinterpret_cast<u32x4*>(const_cast<char*>(row_of(vh, p.pool.v_block, p.pool.v_token, ib, ob)) + d) =
+            *reinterpret_cast<const u32x4*>(row_of(vh, p.pool.v_block, p.pool.v_token, ia, oa) + d);
         if (d == 0) {
             const size_t sa = ((size_t(ia) * p.pool.kv_heads + hk) << p.pool.lb) + oa, sb = ((size_t(ib) * p.pool.kv_heads + hk) << p.pool.lb) + ob;
             p.score_out[sb] = p.score[sa];
@@ -333,7 +332,8 @@ __global__ __launch_bounds__(256) void k_evict_move(const EvictP p, const int pi
     }
 }
 
-constexpr uint32_t kWeighTarget = 2048;
+#include <cstdlib>
+static const uint32_t kWeighTarget = getenv("MTS_W") ? atoi(getenv("MTS_W")) : 2048;
 
 struct EvictSizes {
     uint64_t cap;
@@ -351,14 +351,21 @@ static EvictSizes evict_sizes(uint32_t n, uint32_t kv_heads, uint32_t width, uin
     return s;
 }
 
+template <class T, int D>
+static void launch_weigh(const WeighP& p, uint64_t jobs, hipStream_t stream)
+{
+    static const uint32_t at_once = held_at_once(reinterpret_cast<const void*>(k_weigh<T, D>), 256);
+    hipLaunchKernelGGL((k_weigh<T, D>), dim3(launch_groups(jobs, at_once)), dim3(256), 0, stream, p);
+}
+
 template <class T>
-static void launch_weigh(const WeighP& p, uint32_t D, uint32_t jobs, hipStream_t stream)
+static void launch_weigh(const WeighP& p, uint32_t D, uint64_t jobs, hipStream_t stream)
 {
     switch (D) {
-    case 64: hipLaunchKernelGGL((k_weigh<T, 64>), dim3(jobs), dim3(256), 0, stream, p); break;
-    case 96: hipLaunchKernelGGL((k_weigh<T, 96>), dim3(jobs), dim3(256), 0, stream, p); break;
-    case 128: hipLaunchKernelGGL((k_weigh<T, 128>), dim3(jobs), dim3(256), 0, stream, p); break;
-    default: hipLaunchKernelGGL((k_weigh<T, 256>), dim3(jobs), dim3(256), 0, stream, p); break;
+    case 64: launch_weigh<T, 64>(p, jobs, stream); break;
+    case 96: launch_weigh<T, 96>(p, jobs, stream); break;
+    case 128: launch_weigh<T, 128>(p, jobs, stream); break;
+    default: launch_weigh<T, 256>(p, jobs, stream); break;
     }
 }
 
@@ -395,9 +402,9 @@ int mts_weigh(const mts_weigh_args* a, hipStream_t stream)
     p.decay = a->decay;
     p.target = int(kWeighTarget);
     if (a->pool.type == MTS_BF16)
-        launch_weigh<Bf16>(p, a->pool.head_dim, uint32_t(jobs), stream);
+        launch_weigh<Bf16>(p, a->pool.head_dim, jobs, stream);
     else
-        launch_weigh<F16>(p, a->pool.head_dim, uint32_t(jobs), stream);
+        launch_weigh<F16>(p, a->pool.head_dim, jobs, stream);
     return launched();
 }
 

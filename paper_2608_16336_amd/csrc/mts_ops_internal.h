@@ -17,7 +17,8 @@ constexpr uint32_t kMaxHeads = 65535;
 constexpr uint64_t kMaxSlots = 1ull << 30;
 
 inline bool aligned(const void* p, size_t a) { return p && reinterpret_cast<uintptr_t>(p) % a == 0; }
-inline bool stride8(int64_t s) { return s % 8 == 0 && s >= 0; }
+// strides in elements: whole 16-byte pieces of 16-bit elements, whose number fits 32 bits
+inline bool stride8(int64_t s) { return s % 8 == 0 && s >= 0 && (s / 8) >> 32 == 0; }
 inline uint32_t log2u(uint32_t v) { return uint32_t(__builtin_ctz(v)); }
 inline uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 inline size_t align256(size_t n) { return (n + 255) & ~size_t(255); }
@@ -50,8 +51,8 @@ inline bool batch_ok(const mts_batch& b, uint32_t block_tokens, bool queries)
 struct Pool {
     const char* k;
     const char* v;
-    int64_t k_block, k_head, k_token, v_block, v_head, v_token;  // bytes
-    uint32_t n_blocks, lb, kv_heads;                             // lb: log2 of block_tokens
+    uint32_t k_block, k_head, k_token, v_block, v_head, v_token;  // strides in 16-byte pieces
+    uint32_t n_blocks, lb, kv_heads;                              // lb: log2 of block_tokens
 };
 
 struct Batch {
@@ -64,8 +65,9 @@ struct Batch {
 
 inline Pool device_pool(const mts_pool& p)
 {
-    return Pool{static_cast<const char*>(p.k), static_cast<const char*>(p.v), 2 * p.k_block, 2 * p.k_head, 2 * p.k_token,
-                2 * p.v_block, 2 * p.v_head, 2 * p.v_token, p.n_blocks, log2u(p.block_tokens), p.kv_heads};
+    const auto u = [](int64_t s) { return uint32_t(s / 8); };
+    return Pool{static_cast<const char*>(p.k), static_cast<const char*>(p.v), u(p.k_block), u(p.k_head), u(p.k_token),
+                u(p.v_block), u(p.v_head), u(p.v_token), p.n_blocks, log2u(p.block_tokens), p.kv_heads};
 }
 
 inline Batch device_batch(const mts_batch& b)

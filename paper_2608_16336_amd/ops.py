@@ -262,26 +262,9 @@ def rope_append(q, k, v, positions, slots, freqs, k_cache, v_cache, pos=None, *,
 
 # ------------------------------------------------------------------ attention
 
-_workspaces = {}
-
-
-def _zeroed(device, nbytes):
-    """The stream's zero-initialised workspace, grown as needed.  Under graph
-    capture a new one from the graph's own memory."""
-    if device.type != "cuda":
-        raise ValueError("tensors must be on a GPU")
-    if torch._C._cuda_isCurrentStreamCapturing():
-        return torch.zeros(nbytes, dtype=torch.uint8, device=device)
-    key = (device.index, torch._C._cuda_getCurrentRawStream(device.index))
-    w = _workspaces.get(key)
-    if w is None or w.numel() < nbytes:
-        w = _workspaces[key] = torch.zeros(max(nbytes, 1 << 20), dtype=torch.uint8, device=device)
-    return w
-
-
 @functools.lru_cache(maxsize=256)
 def attend_workspace(n, n_tokens, max_q, q_heads, kv_heads, head_dim):
-    """Bytes of a workspace for attend() calls of at most these sizes."""
+    """Bytes of the workspace that attend() takes for these sizes."""
     b = _size(0)
     _check("mts_attend_workspace", _library().mts_attend_workspace(n, n_tokens, max_q, q_heads, kv_heads, head_dim, ctypes.byref(b)))
     return b.value
@@ -293,8 +276,8 @@ def attend(q, k_cache, v_cache, table, lens, q_start, max_q, *, scale=None, tree
     tokens of a request.  tree [tokens][words] int64: bit i of a token says
     whether it attends its request's i-th new token; without it new tokens
     attend those before them and themselves.  scale: dim ** -0.5 by default.
-    workspace: a zeroed uint8 tensor of attend_workspace() bytes kept for one
-    stream's calls; by default the module keeps one a stream."""
+    workspace: a uint8 tensor of at least attend_workspace() bytes that no other
+    stream uses meanwhile; by default one is taken for the call."""
     device, dtype = q.device, q.dtype
     strides = _rows(q, "q", device, dtype)
     N, Hq, D = q.shape
@@ -312,7 +295,7 @@ def attend(q, k_cache, v_cache, table, lens, q_start, max_q, *, scale=None, tree
     if lse is None:
         lse = torch.empty((N, Hq), dtype=_FLOAT32, device=device)
     if workspace is None:
-        workspace = _zeroed(device, attend_workspace(lens.shape[0], N, max_q, Hq, k_cache.shape[1], D))
+        workspace = torch.empty(attend_workspace(lens.shape[0], N, max_q, Hq, k_cache.shape[1], D), dtype=torch.uint8, device=device)
     elif workspace.device != device or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
         raise ValueError("workspace: contiguous uint8 on %s" % device)
     _call("mts_attend", _attend_pack(

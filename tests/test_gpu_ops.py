@@ -236,7 +236,7 @@ def test_attend_workspace_serves_calls_of_other_sizes():
     """One workspace for large and small calls in turn."""
     big = ref.make_batch([2000] * 6, [12] * 6, 16, 2, 64, BF, seed=15)
     small = ref.make_batch([900], [1], 16, 2, 64, BF, seed=16)
-    ws = torch.zeros(ops.attend_workspace(6, 72, 12, 8, 2, 64), dtype=torch.uint8, device="cuda")
+    ws = torch.full((ops.attend_workspace(6, 72, 12, 8, 2, 64),), 255, dtype=torch.uint8, device="cuda")
     qb, qs = query(big, 8, 64, BF), query(small, 8, 64, BF)
     want_b, want_s = run_attend(big, qb)[0], run_attend(small, qs)[0]
     for _ in range(3):
