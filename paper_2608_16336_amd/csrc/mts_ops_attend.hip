@@ -1,6 +1,4 @@
 // Attention of new tokens over a paged cache (mts_attend).
-#include <type_traits>
-
 #include "mts_ops_dev.h"
 
 namespace mts {
@@ -356,9 +354,6 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void k_attend_rows(const Att
 // and added to the rows that see them, which is what weighting them gives.
 constexpr float kSlack = 8.f;
 constexpr float kLowest = -3.0e38f;  // below any score's power of two
-
-template <int N>
-using Int = std::integral_constant<int, N>;
 
 template <class T, int D, int NW>
 __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void k_attend_tiles(const AttendP p)

@@ -10,6 +10,8 @@
 //             pieces of 4 elements; lane i gets column i of the 4 rows
 #pragma once
 
+#include <type_traits>
+
 #include <hip/hip_runtime.h>
 
 #include "mts_ops_internal.h"
@@ -28,6 +30,9 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+template <int N>
+using Int = std::integral_constant<int, N>;
 
 struct Bf16 {
     using e = __bf16;

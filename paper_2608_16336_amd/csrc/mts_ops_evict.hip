@@ -25,7 +25,7 @@ constexpr int kWeighRound = 128;  // keys of one round of a workgroup: 4 waves x
 // 16 keys of one query: weights add up in the lane, and over the 32 lanes at
 // the end, where each step of the exchange halves what a lane still holds.
 template <class T, int D>
-__global__ __launch_bounds__(256, D == 256 ? 2 : 4) void k_weigh(const WeighP p)
+__global__ __launch_bounds__(256, D == 256 ? 2 : 3) void k_weigh(const WeighP p)
 {
     constexpr int KS = D / 16, CH = D / 8, ROWS = D == 256 ? 64 : 128;
     __shared__ __attribute__((aligned(16))) char qs[ROWS * D * 2];
@@ -43,6 +43,7 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 4) void k_weigh(const WeighP p)
         // rows [row0, row0 + ROWS) and their lse in powers of two; rows past the end and rows that saw nothing get +inf
         const auto stage = [&](int row0) {
             __syncthreads();
+#pragma unroll 1
             for (int i = tid; i < ROWS * CH; i += 256) {
                 const int row = i / CH, piece = i % CH, at = row0 + row;
                 if (row0 + (row & ~31) >= rows) break;
@@ -58,23 +59,32 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 4) void k_weigh(const WeighP p)
             }
             __syncthreads();
         };
-        if (rows <= ROWS) stage(0);
-        // block ids are read a tile ahead of its keys
-        int next;
+        // a tile's keys are asked for while the one before is computed, its block ids another tile earlier
+        int next, id_next;
+        s16x8 kn[KS];
         const auto load_id = [&](int k0) { next = k0 + lq < j.k1 ? p.batch.table[size_t(j.r) * p.batch.width + ((k0 + lq) >> p.pool.lb)] : -1; };
-        load_id(j.k0 + 32 * w);
-        for (int kr = j.k0; kr < j.k1; kr += kWeighRound) {
-            const int k0 = kr + 32 * w;
-            const int id = unsigned(next) < p.pool.n_blocks ? next : -1;
-            s16x8 kf[KS];
-            const char* kp = row_of(kh, p.pool.k_block, p.pool.k_token, max(id, 0), id < 0 ? 0 : (k0 + lq) & omask);
+        const auto load_keys = [&](int k0) {
+            id_next = unsigned(next) < p.pool.n_blocks ? next : -1;
+            const char* kp = row_of(kh, p.pool.k_block, p.pool.k_token, max(id_next, 0), id_next < 0 ? 0 : (k0 + lq) & omask);
 #pragma unroll
-            for (int s = 0; s < KS; ++s) kf[s] = *reinterpret_cast<const s16x8*>(kp + (2 * s + h) * 16);
+            for (int s = 0; s < KS; ++s) kn[s] = *reinterpret_cast<const s16x8*>(kp + (2 * s + h) * 16);
             load_id(k0 + kWeighRound);
+        };
+        load_id(j.k0 + 32 * w);
+        load_keys(j.k0 + 32 * w);
+        if (rows <= ROWS) stage(0);
+        for (int kr = j.k0; kr < j.k1; kr += kWeighRound) {
+            const int k0 = kr + 32 * w, id = id_next;
+            s16x8 kf[KS];
+#pragma unroll
+            for (int s = 0; s < KS; ++s) kf[s] = kn[s];
+            if (kr + kWeighRound < j.k1) load_keys(k0 + kWeighRound);
             float acc[16] = {};
             const bool fresh = k0 + 32 > base;
+#pragma unroll 1
             for (int row0 = 0; row0 < rows; row0 += ROWS) {
                 if (rows > ROWS) stage(row0);
+#pragma unroll 1
                 for (int r = 0; r < ROWS && row0 + r < rows; r += 32) {
                     const float ref = refs[r + lq];
                     f32x16 sc;
@@ -101,17 +111,21 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 4) void k_weigh(const WeighP p)
                 }
             }
             // bit 4 of the lane's number keeps the upper or lower eight sums, bit 3 of these the upper or lower four, ...
+            // (sums 8 and 4 stand for keys 16 and 8, sums 2 and 1 for keys 2 and 1)
             int key = k0 + 4 * h;
-#pragma unroll
-            for (int o = 16, n = 8; n; o >>= 1, n >>= 1) {
-                const bool up = lane & o;
+            const auto halve = [&](auto bit, auto n, auto keys) {
+                const bool up = lane & bit;
 #pragma unroll
                 for (int i = 0; i < n; ++i) {
                     const float keep = up ? acc[n + i] : acc[i], give = up ? acc[i] : acc[n + i];
-                    acc[i] = keep + __shfl_xor(give, o);
+                    acc[i] = keep + __shfl_xor(give, bit);
                 }
-                key += up ? (n >= 4 ? 2 * n : n) : 0;  // sums 8 and 4 stand for keys 16 and 8, sums 2 and 1 for keys 2 and 1
-            }
+                key += up ? keys : 0;
+            };
+            halve(Int<16>(), Int<8>(), Int<16>());
+            halve(Int<8>(), Int<4>(), Int<8>());
+            halve(Int<4>(), Int<2>(), Int<2>());
+            halve(Int<2>(), Int<1>(), Int<1>());
             const float mine = acc[0] + __shfl_xor(acc[0], 1);
             const int block = __shfl(id, (key - k0) & 31);  // the lane that loaded the key knows its block
             if (!(lane & 1) && block >= 0) {
@@ -332,8 +346,10 @@ __global__ __launch_bounds__(256) void k_evict_move(const EvictP p, const int pi
     }
 }
 
-#include <cstdlib>
-static const uint32_t kWeighTarget = getenv("MTS_W") ? atoi(getenv("MTS_W")) : 2048;
+// Jobs to aim for, three a compute unit as the chip holds (a decode step's
+// weights of 150 requests take 62, 63, 66, 65, 67 us at 512, 768, 1024, 1536,
+// 2048; those of six windows of 64 tokens 84, 69, 98, 71, 72 us).
+constexpr uint32_t kWeighTarget = 768;
 
 struct EvictSizes {
     uint64_t cap;

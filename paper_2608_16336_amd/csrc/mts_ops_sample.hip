@@ -14,11 +14,10 @@ struct SampleP {
     int vocab, frac;  // frac: bits below the point of a summed weight
 };
 
-constexpr int kThreads = 1024, kWaves = 16;
 typedef unsigned long long u64;
 
 // A row as 16-byte vectors from the aligned address at or below its start;
-// elements outside the row read as -inf with a key below all others'.
+// elements outside the row read as -inf.
 template <class E>
 struct Row {
     static constexpr int N = 16 / int(sizeof(E));
@@ -37,53 +36,70 @@ struct Row {
     }
     // index of element 0 of vector i
     __device__ __forceinline__ int first(int i) const { return i * N - skip; }
-    __device__ __forceinline__ void load(int i, float x[N]) const
+    __device__ __forceinline__ V raw(int i) const
     {
         const int f = first(i);
-        if (f >= 0 && f + N <= vocab) {
-            const V v = *reinterpret_cast<const V*>(start + 16 * size_t(i));
+        if (f >= 0 && f + N <= vocab) return *reinterpret_cast<const V*>(start + 16 * size_t(i));
+        V v;
 #pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = float(v.e[e]);
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                x[e] = f + e >= 0 && f + e < vocab ? float(*reinterpret_cast<const E*>(start + 16 * size_t(i) + e * sizeof(E))) : -__builtin_inff();
-        }
-#pragma unroll
-        for (int e = 0; e < N; ++e) x[e] = x[e] != x[e] ? -__builtin_inff() : x[e] + 0.f;
+        for (int e = 0; e < N; ++e)
+            v.e[e] = f + e >= 0 && f + e < vocab ? *reinterpret_cast<const E*>(start + 16 * size_t(i) + e * sizeof(E)) : E(-__builtin_inff());
+        return v;
     }
+    // NaN as -inf
+    __device__ __forceinline__ void widen(const V& v, float x[N]) const
+    {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float f = float(v.e[e]);
+            x[e] = f != f ? -__builtin_inff() : f;
+        }
+    }
+    __device__ __forceinline__ void load(int i, float x[N]) const { widen(raw(i), x); }
 };
 
 __device__ __forceinline__ unsigned logit_key(float x)
 {
-    const unsigned u = __float_as_uint(x);
+    const unsigned u = __float_as_uint(x + 0.f);  // -0 as 0
     return u ^ (u >> 31 ? 0xffffffffu : 0x80000000u);
 }
+__device__ __forceinline__ float key_logit(unsigned k) { return __uint_as_float(k ^ (k >> 31 ? 0x80000000u : 0xffffffffu)); }
 
 // Weights are summed as whole numbers of 2^-frac, to the nearest: the sums do
 // not depend on any order, and are off by less than 2^-frac a token.  Adding
 // 1.5 * 2^(52 - frac) leaves the rounded number in the low bits of the double.
 struct Weigher {
-    float top, inv_t, min_w;
+    float top, inv_t;  // finite: an infinite logit counts as the largest number, and the distance from it as 0
     double magic;
     u64 magic_bits;
-    __device__ __forceinline__ float weight(float x) const
-    {
-        return x == top ? 1.f : x == -__builtin_inff() ? 0.f : expf((x - top) * inv_t);
-    }
-    __device__ __forceinline__ u64 fixed(float w) const { return u64(__double_as_longlong(double(w) + magic)) - magic_bits; }
+    // distance from the top, <= 0, in powers of e
+    __device__ __forceinline__ float distance(float x) const { return (fminf(x, __FLT_MAX__) - top) * inv_t; }
+    __device__ __forceinline__ float weight(float x) const { return expf(distance(x)); }
+    // magic_bits + the rounded number; sums of these have magic_bits taken off afterwards, once for each
+    __device__ __forceinline__ u64 biased(float w) const { return u64(__double_as_longlong(double(w) + magic)); }
+    __device__ __forceinline__ u64 fixed(float w) const { return biased(w) - magic_bits; }
 };
 
-template <class F>
-__device__ __forceinline__ u64 block_sum64(u64 v, F* scratch)
+// Sum over the lower threads of a workgroup, and the total.
+template <int kWaves>
+__device__ __forceinline__ u64 block_before(u64 v, u64& total, u64* scratch)
 {
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    u64 incl = v;
+    for (int o = 1; o < 64; o <<= 1) {
+        const u64 u = __shfl_up(incl, o);
+        if (lane >= o) incl += u;
+    }
     __syncthreads();
-    if ((threadIdx.x & 63) == 0) scratch[threadIdx.x >> 6] = v;
+    if (lane == 63) scratch[w] = incl;
     __syncthreads();
-    u64 s = 0;
-    for (int i = 0; i < kWaves; ++i) s += scratch[i];
-    return s;
+    u64 before = incl - v;
+    total = 0;
+    for (int i = 0; i < kWaves; ++i) {
+        if (i < w) before += scratch[i];
+        total += scratch[i];
+    }
+    return before;
 }
 
 __device__ __forceinline__ u64 wave_incl(u64 v)
@@ -96,247 +112,468 @@ __device__ __forceinline__ u64 wave_incl(u64 v)
     return v;
 }
 
-// One workgroup a row.  The kept set is a threshold key with a count of the
-// lowest-numbered tokens of that key, found by radix selection over 11, 11 and
-// 10 bits of the key: by counts for top-k, by summed weights for top-p.
-template <class E>
-__global__ __launch_bounds__(kThreads) void k_sample(const SampleP p)
-{
-    constexpr int N = Row<E>::N;
-    __shared__ u64 hist[2048];
-    __shared__ u64 scratch[kWaves];
-    __shared__ u64 cut_sum;
-    __shared__ int cut_bin;
-    __shared__ unsigned wave_top[kWaves];
-    __shared__ int wave_n[kWaves];
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const Row<E> row(p.logits + b * p.row_bytes, p.vocab);
+constexpr int kBins = 2048;
+// tokens that are ranked one by one (each against all: 256 take about a microsecond), and the largest top-k whose ranks
+// are looked for among that many
+constexpr int kCandidates = 512, kFew = 256;
 
-    // the largest key and its lowest index
-    unsigned best = 0;
-    int at = 0x7fffffff;
-    for (int i = tid; i < row.nvec; i += kThreads) {
-        float x[N];
-        row.load(i, x);
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const unsigned k = logit_key(x[e]);
-            if (k > best) best = k, at = row.first(i) + e;
+// The last rank that a rule keeps: its key and its index.
+struct Cut {
+    unsigned key;
+    int index;
+};
+
+template <class E, int kWaves>
+struct Sampler {
+    static constexpr int N = Row<E>::N, kThreads = 64 * kWaves, kEach = kBins / kThreads;  // bins a thread
+    struct Shared {
+        u64 sum[kBins];
+        u64 c_order[kCandidates], c_share[kCandidates];  // see order(); what the rule sums
+        u64 r_order[kCandidates], r_share[kCandidates];  // the same by rank
+        u64 scratch[kWaves];
+        u64 above;
+        unsigned lo, hi;
+        int bin, n, best, index;
+    };
+    const Row<E>& row;
+    const Weigher& wt;
+    Shared& sh;
+    int v0, v1;  // the wave's vectors: consecutive, so that waves, vectors and lanes are in vocabulary order
+    Cut within;  // what rules before this one have kept
+
+    // f(index of the vector's element 0, its elements) for the wave's vectors, with three loads on their way
+    template <class F>
+    __device__ __forceinline__ void each(F f) const
+    {
+        typename Row<E>::V a{}, b{}, c{};
+        const int i0 = v0 + int(threadIdx.x & 63);
+        if (i0 < v1) a = row.raw(i0);
+        if (i0 + 64 < v1) b = row.raw(i0 + 64);
+        if (i0 + 128 < v1) c = row.raw(i0 + 128);
+#pragma unroll 1
+        for (int i = i0; i < v1; i += 64) {
+            float x[N];
+            row.widen(a, x);
+            a = b;
+            b = c;
+            if (i + 192 < v1) c = row.raw(i + 192);
+            f(row.first(i), x);
         }
     }
+    __device__ __forceinline__ bool in(const Cut& c, int index, unsigned k) const { return k > c.key || (k == c.key && index <= c.index); }
+
+    // Bins by the distance from the top, 128 a factor of e: most of a row's tokens lie within a few dozen factors, so a
+    // wave's lanes seldom meet in a bin.
+    __device__ __forceinline__ float bins_down(float x) const { return fminf(wt.distance(x) * -128.f, float(kBins - 1)); }
+
+    __device__ __forceinline__ void clear()
+    {
+        __syncthreads();
+        for (int i = threadIdx.x; i < kBins; i += kThreads) sh.sum[i] = 0;
+        __syncthreads();
+    }
+    // what a rule sums: ranks, or weights
+    __device__ __forceinline__ u64 share(bool by_mass, float x) const { return by_mass ? wt.fixed(wt.weight(x)) : 1; }
+
+    // Larger for an earlier rank: by key, equal ones by index.
+    static __device__ __forceinline__ u64 order(unsigned key, int index) { return u64(key) << 32 | unsigned(0x7fffffff - index); }
+    static __device__ __forceinline__ unsigned order_key(u64 o) { return unsigned(o >> 32); }
+    static __device__ __forceinline__ int order_index(u64 o) { return 0x7fffffff - int(unsigned(o)); }
+
+    // The listed tokens by rank; returns how many there are.
+    __device__ __forceinline__ int rank_listed()
+    {
+        const int n = sh.n, t = threadIdx.x;
+        if (t < n) {
+            const u64 mine = sh.c_order[t];
+            int rank = 0;
+            for (int i = 0; i < n; ++i) rank += sh.c_order[i] > mine;
+            sh.r_order[rank] = mine;
+            sh.r_share[rank] = sh.c_share[t];
+        }
+        __syncthreads();
+        return n;
+    }
+
+    // Finds the bin that the cut lies in: the last one with anything in it whose first rank is kept, ranks being kept while
+    // the sum before them is below the limit.  sh.above: what comes before it, counted on from what it holds.
+    __device__ __forceinline__ bool begins(u64 s, double limit) const { return s == 0 || double(s) < limit; }
+    __device__ __forceinline__ void find_bin(double limit)
+    {
+        const int b = kEach * threadIdx.x;
+        u64 x[kEach], mine = 0, total;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) mine += x[i] = sh.sum[b + i];
+        if (threadIdx.x == 0) sh.bin = -1;
+        u64 before = sh.above + block_before<kWaves>(mine, total, sh.scratch);
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) {
+            if (x[i] && begins(before, limit)) atomicMax(&sh.bin, b + i);
+            before += x[i];
+        }
+        __syncthreads();
+        const int bin = sh.bin;
+#pragma unroll
+        for (int i = kEach - 1; i >= 0; --i) {
+            before -= x[i];
+            if (bin == b + i) sh.above = before;
+        }
+        __syncthreads();
+    }
+
+    // The last rank kept, ranks being kept while the sum before them (of ranks, or of weights) is below the limit.  The
+    // bins of the whole row are filled; where more tokens share the cut's bin than can be ranked one by one, it is divided
+    // by keys, 2048 ways at a time.
+    __device__ __forceinline__ Cut find(bool by_mass, double limit)
+    {
+        __syncthreads();
+        if (threadIdx.x == 0) sh.above = 0;
+        __syncthreads();
+        find_bin(limit);
+        const float bin = float(sh.bin), next = sh.bin == kBins - 1 ? __builtin_inff() : bin + 1.f;
+        unsigned lo = 0, hi = 0xffffffffu;  // what is left: this bin's tokens whose keys lie between
+        const auto left = [&](int index, float x, unsigned k) {
+            const float d = bins_down(x);
+            return d >= bin && d < next && k >= lo && k <= hi && in(within, index, k);
+        };
+        for (;;) {
+            // list what is left as far as it fits, and its smallest and largest key
+            if (threadIdx.x == 0) sh.n = 0, sh.best = -1, sh.lo = 0xffffffffu, sh.hi = 0;
+            __syncthreads();
+            unsigned least = 0xffffffffu, most = 0;
+            each([&](int f, const float x[N]) {
+                unsigned some = 0;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const float d = bins_down(x[e]);
+                    some |= unsigned(d >= bin && d < next) << e;
+                }
+                if (!some) return;
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if (!((some >> e) & 1) || unsigned(f + e) >= unsigned(row.vocab)) continue;
+                    const unsigned k = logit_key(x[e]);
+                    if (!left(f + e, x[e], k)) continue;
+                    least = min(least, k);
+                    most = max(most, k);
+                    const int at = atomicAdd(&sh.n, 1);
+                    if (at >= kCandidates) continue;
+                    sh.c_order[at] = order(k, f + e);
+                    sh.c_share[at] = share(by_mass, x[e]);
+                }
+            });
+            if (most >= least) atomicMin(&sh.lo, least), atomicMax(&sh.hi, most);
+            __syncthreads();
+            if (sh.n <= kCandidates) break;
+            lo = sh.lo;
+            hi = sh.hi;
+            if (lo == hi) return find_equal(by_mass, limit, lo);
+            const int shift = max(0, 32 - __clz(int(hi - lo)) - 11);
+            clear();
+            each([&](int f, const float x[N]) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    const unsigned k = logit_key(x[e]);
+                    if (left(f + e, x[e], k)) atomicAdd(&sh.sum[(hi - k) >> shift], share(by_mass, x[e]));
+                }
+            });
+            __syncthreads();
+            find_bin(limit);
+            hi -= unsigned(sh.bin) << shift;
+            const unsigned width = (1u << shift) - 1;
+            lo = hi - lo > width ? hi - width : lo;
+        }
+        const int n = rank_listed(), t = threadIdx.x;
+        u64 total;
+        const u64 above = sh.above, before = above + block_before<kWaves>(t < n ? sh.r_share[t] : 0, total, sh.scratch);
+        if (t < n && begins(before, limit)) atomicMax(&sh.best, t);
+        __syncthreads();
+        const u64 last = sh.r_order[sh.best];
+        __syncthreads();
+        return Cut{order_key(last), order_index(last)};
+    }
+
+    // Where the kept tokens are few they are found without bins of the whole row, and the token is drawn from their list.
+    // `most` is the largest logit that this thread has met: as many of the threads' largest as there are ranks wanted are
+    // at or above some bin, hence at least so many tokens are, and seldom many more.  They are listed in one pass, with
+    // the sum of all weights where top-p asks for it.  Returns false if they do not fit or do not reach the share that
+    // top-p keeps.
+    __device__ __forceinline__ bool draw_few(float most, int k, float top_p, float min_w, float u, int frac, int32_t* token, float* logprob)
+    {
+        const bool by_p = top_p < 1.f;
+        const int t = threadIdx.x;
+        clear();
+        if (t == 0) sh.above = 0, sh.n = 0, sh.best = -1;
+        atomicAdd(&sh.sum[int(bins_down(most))], 1ull);
+        __syncthreads();
+        find_bin(double(k ? k : kFew - 64));
+        const float next = sh.bin == kBins - 1 ? __builtin_inff() : float(sh.bin + 1);
+        u64 z = 0;
+        each([&](int f, const float x[N]) {
+            float m = x[0];
+#pragma unroll
+            for (int e = 1; e < N; ++e) m = fmaxf(m, x[e]);
+            if (bins_down(m) < next) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    // (what lies outside the row reads as -inf and would be listed for it)
+                    if (!(bins_down(x[e]) < next) || unsigned(f + e) >= unsigned(row.vocab)) continue;
+                    const int at = atomicAdd(&sh.n, 1);
+                    if (at >= kCandidates) continue;
+                    sh.c_order[at] = order(logit_key(x[e]), f + e);
+                    sh.c_share[at] = wt.fixed(wt.weight(x[e]));
+                }
+            }
+            if (by_p && !k) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) z += wt.biased(wt.weight(x[e]));
+                z -= u64(N) * wt.magic_bits;
+            }
+        });
+        __syncthreads();
+        if (sh.n > kCandidates) return false;
+        const int n = rank_listed();
+        u64 total, all, W;
+        const u64 share = t < n && (!k || t < k) ? sh.r_share[t] : 0;
+        const u64 before = block_before<kWaves>(share, total, sh.scratch);
+        bool keep = t < n && (!k || t < k);
+        if (by_p) {
+            if (k)
+                all = total;
+            else
+                (void)block_before<kWaves>(z, all, sh.scratch);
+            const double limit = double(top_p) * double(all);
+            if (!k && double(total) < limit) return false;
+            keep = keep && begins(before, limit);
+        }
+        const u64 order_t = t < n ? sh.r_order[t] : 0;
+        const float w = t < n ? wt.weight(key_logit(order_key(order_t))) : 0.f;
+        keep = keep && w >= min_w;
+        // kept ranks are the first ones: their sum in vocabulary order up to each
+        (void)block_before<kWaves>(keep ? share : 0, W, sh.scratch);
+        if (keep) atomicMax(&sh.best, t);
+        __syncthreads();
+        const int kept = sh.best + 1;
+        const double target = double(fmaxf(u, 0.f)) * double(W);
+        if (t < kept) {
+            u64 upto = 0;
+            const unsigned me = unsigned(order_t);
+            for (int i = 0; i < kept; ++i) upto += unsigned(sh.r_order[i]) >= me ? sh.r_share[i] : 0;
+            // the first that exceeds the target; u of 1 and more ends at the last with any weight
+            const bool hit = share && !(double(upto - share) > target) && (double(upto) > target || upto == W);
+            if (hit) {
+                *token = order_index(order_t);
+                if (logprob) *logprob = float(log(ldexp(double(w), frac) / double(W)));
+            }
+        }
+        return true;
+    }
+
+    // The cut where all that is left has the same key: so many of the lowest-numbered ones.
+    __device__ __forceinline__ Cut find_equal(bool by_mass, double limit, unsigned key)
+    {
+        const u64 one = share(by_mass, key_logit(key));
+        const double more = one ? ceil((limit - double(sh.above)) / double(one)) : 1.0;
+        const u64 need = more < 1.0 ? 1 : more < double(sh.n) ? u64(more) : u64(sh.n);
+        u64 eq = 0;
+        const auto equals = [&](int f, const float x[N]) {
+            int n = 0;
+#pragma unroll
+            for (int e = 0; e < N; ++e) n += logit_key(x[e]) == key && in(within, f + e, key);
+            return n;
+        };
+        each([&](int f, const float x[N]) { eq += equals(f, x); });
+        for (int o = 32; o; o >>= 1) eq += __shfl_xor(eq, o);
+        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+        __syncthreads();
+        if (lane == 0) sh.scratch[w] = eq;
+        __syncthreads();
+        u64 before = 0;
+        for (int i = 0; i < w; ++i) before += sh.scratch[i];
+        if (before < need && need <= before + eq) {
+            for (int i = v0; i < v1; i += 64) {
+                float x[N];
+                int n = 0;
+                if (i + lane < v1) {
+                    row.load(i + lane, x);
+                    n = equals(row.first(i + lane), x);
+                }
+                const u64 incl = wave_incl(u64(n)), at = before + incl - n;
+                if (at < need && need <= at + n) {
+                    u64 c = at;
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (logit_key(x[e]) == key && in(within, row.first(i + lane) + e, key) && ++c == need) sh.index = row.first(i + lane) + e;
+                }
+                before += __shfl(incl, 63);
+                if (before >= need) break;
+            }
+        }
+        __syncthreads();
+        return Cut{key, sh.index};
+    }
+};
+
+// One workgroup a row: the largest logit; where a rule asks for it counts and
+// weights in bins by distance from it, and the cuts; the kept weights of each
+// wave's stretch of the row; the stretch that the random number falls in.  The
+// row is read four to six times, after the first from the caches: no more of
+// 512 rows of 200 KB fits the registers, and passes unrolled over registers
+// would not fit the instruction cache.
+template <class E, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 4) void k_sample(const SampleP p)
+{
+    constexpr int N = Row<E>::N;
+    using S = Sampler<E, kWaves>;
+    __shared__ typename S::Shared sh;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const Row<E> row(p.logits + b * p.row_bytes, p.vocab);
+    const int seg = ((row.nvec + kWaves * 64 - 1) / (kWaves * 64)) * 64;
+    const int v0 = min(w * seg, row.nvec), v1 = min(v0 + seg, row.nvec);
+    Weigher wt;
+    S s{row, wt, sh, v0, v1, Cut{0, 0x7fffffff}};
+
+    // the largest logit and its lowest index
+    float best = -__builtin_inff();
+    int at = 0x7fffffff;
+    s.each([&](int f, const float x[N]) {
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (x[e] > best) best = x[e], at = f + e;
+    });
+    const float most = best;  // of this thread
     for (int o = 32; o; o >>= 1) {
-        const unsigned k = __shfl_xor(best, o);
+        const float k = __shfl_xor(best, o);
         const int a = __shfl_xor(at, o);
         if (k > best || (k == best && a < at)) best = k, at = a;
     }
-    if (lane == 0) wave_top[w] = best, wave_n[w] = at;
+    if (lane == 0) sh.c_share[w] = u64(__float_as_uint(best)) << 32 | unsigned(at);
     __syncthreads();
-    for (int i = 0; i < kWaves; ++i)
-        if (wave_top[i] > best || (wave_top[i] == best && wave_n[i] < at)) best = wave_top[i], at = wave_n[i];
+    for (int i = 0; i < kWaves; ++i) {
+        const float k = __uint_as_float(unsigned(sh.c_share[i] >> 32));
+        const int a = int(unsigned(sh.c_share[i]));
+        if (k > best || (k == best && a < at)) best = k, at = a;
+    }
+    __syncthreads();
     const float t = p.temperature[b];
-    if (best <= logit_key(-__builtin_inff()) || !(t > 0.f)) {
-        const bool dead = best <= logit_key(-__builtin_inff());
+    const bool dead = best == -__builtin_inff();
+    if (dead || !(t > 0.f)) {
         if (tid == 0) {
             p.token[b] = dead ? -1 : at;
             if (p.logprob) p.logprob[b] = dead ? -__builtin_inff() : 0.f;
         }
         return;
     }
-    Weigher wt;
-    wt.top = __uint_as_float(best ^ (best >> 31 ? 0x80000000u : 0xffffffffu));
-    wt.inv_t = 1.f / t;
-    wt.min_w = fminf(fmaxf(p.min_p[b], 0.f), 1.f);  // the first rank always stays
+    wt.top = fminf(best, __FLT_MAX__);
+    wt.inv_t = fminf(fmaxf(1.f / t, __FLT_MIN__), __FLT_MAX__);
     wt.magic = ldexp(1.5, 52 - p.frac);
     wt.magic_bits = u64(__double_as_longlong(wt.magic));
+    const float min_w = fminf(fmaxf(p.min_p[b], 0.f), 1.f);  // the first rank always stays
 
-    // kept: keys above thr, and the `need` lowest-numbered of those equal to it
-    unsigned thr = 0;
-    u64 need = ~0ull;
-    const int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
+    // top-k by ranks, then top-p by the weights of what is left
     const int k_top = p.top_k[b];
     const float top_p = p.top_p[b];
-    const bool by_k = k_top > 0 && k_top < p.vocab, by_p = top_p < 1.f;
+    const bool by_k = k_top > 0 && k_top < p.vocab;
+    if ((by_k ? k_top <= kFew : top_p < 1.f) &&
+        s.draw_few(most, by_k ? k_top : 0, top_p, min_w, p.u[b], p.frac, p.token + b, p.logprob ? p.logprob + b : nullptr))
+        return;
+    bool cuts = false;
+#pragma unroll 1
     for (int rule = 0; rule < 2; ++rule) {
-        if (!(rule ? by_p : by_k)) continue;
-        // rule 0: the first k_top ranks; rule 1: ranks while the weight before them is below the limit
-        const unsigned old_thr = thr;
-        const u64 old_need = need;
-        double limit = 0.0;
+        if (!(rule ? top_p < 1.f : by_k)) continue;
+        s.clear();
+        s.each([&](int f, const float x[N]) {
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (!cuts || s.in(s.within, f + e, logit_key(x[e]))) atomicAdd(&sh.sum[int(s.bins_down(x[e]))], s.share(rule, x[e]));
+        });
+        __syncthreads();
+        double limit = double(k_top);
         if (rule) {
-            u64 z = 0, eq = 0;
-            for (int i = tid; i < row.nvec; i += kThreads) {
-                float x[N];
-                row.load(i, x);
+            u64 z, mine = 0;
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const unsigned k = logit_key(x[e]);
-                    if (k > old_thr || (k == old_thr && old_need == ~0ull)) z += wt.fixed(wt.weight(x[e]));
-                }
-            }
-            z = block_sum64(z, scratch);
-            if (old_need != ~0ull) {
-                const float x = __uint_as_float(old_thr ^ (old_thr >> 31 ? 0x80000000u : 0xffffffffu));
-                eq = old_need * wt.fixed(wt.weight(x));
-            }
-            limit = double(top_p) * double(z + eq);
+            for (int i = 0; i < S::kEach; ++i) mine += sh.sum[S::kEach * tid + i];
+            (void)block_before<kWaves>(mine, z, sh.scratch);
+            limit = double(top_p) * double(z);
         }
-        unsigned found = 0, mask = 0;
-        u64 above = 0;  // counts or weights of the keys above the found prefix
-        for (int d = 0; d < 3; ++d) {
-            const int n = 1 << bits[d];
-            __syncthreads();
-            hist[tid] = 0;
-            hist[tid + 1024] = 0;
-            if (tid == 0) cut_bin = -1;
-            __syncthreads();
-            for (int i = tid; i < row.nvec; i += kThreads) {
-                float x[N];
-                row.load(i, x);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const unsigned k = logit_key(x[e]);
-                    const int f = row.first(i) + e;
-                    if (f < 0 || f >= p.vocab || (k & mask) != found || k < old_thr) continue;
-                    atomicAdd(&hist[(k >> shifts[d]) & (n - 1)], rule ? wt.fixed(wt.weight(x[e])) : 1ull);
-                }
-            }
-            __syncthreads();
-            const int hi = n - 1 - 2 * tid, lo = hi - 1;
-            const u64 a = hi >= 0 ? hist[hi] : 0, c = lo >= 0 ? hist[lo] : 0;
-            const u64 incl = wave_incl(a + c);
-            if (lane == 63) scratch[w] = incl;
-            __syncthreads();
-            u64 before = above;
-            for (int i = 0; i < w; ++i) before += scratch[i];
-            before += incl - a - c;
-            // the last bin with anything in it whose ranks begin below the limit
-            const auto below = [&](u64 s) { return rule ? s == 0 || double(s) < limit : s < u64(k_top); };
-            if (a && below(before)) atomicMax(&cut_bin, 2047 - hi);
-            if (c && below(before + a)) atomicMax(&cut_bin, 2047 - lo);
-            __syncthreads();
-            const int bin = 2047 - cut_bin;
-            if (bin == hi && a) cut_sum = before;
-            if (bin == lo && c) cut_sum = before + a;
-            __syncthreads();
-            above = cut_sum;
-            found |= unsigned(bin) << shifts[d];
-            mask |= unsigned(n - 1) << shifts[d];
-        }
-        thr = found;
-        if (!rule) {
-            need = u64(k_top) - above;
-        } else {
-            const float x = __uint_as_float(thr ^ (thr >> 31 ? 0x80000000u : 0xffffffffu));
-            const u64 one = wt.fixed(wt.weight(x));
-            // how many of the equal ones begin below the limit
-            double more = one ? ceil((limit - double(above)) / double(one)) : 1.0;
-            more = more < 1.0 ? 1.0 : more;
-            need = more < 16777216.0 ? u64(more) : 16777216ull;
-            if (thr == old_thr && old_need < need) need = old_need;
-        }
+        s.within = s.find(rule, limit);
+        cuts = true;
     }
 
-    // waves own consecutive stretches of the row
-    const int seg = ((row.nvec + kWaves * 64 - 1) / (kWaves * 64)) * 64;
-    const int v0 = min(w * seg, row.nvec), v1 = min(v0 + seg, row.nvec);
-    u64 eq_before = 0;
-    if (need != ~0ull) {
-        u64 eq = 0;
-        for (int i = v0 + lane; i < v1; i += 64) {
-            float x[N];
-            row.load(i, x);
-#pragma unroll
-            for (int e = 0; e < N; ++e) eq += logit_key(x[e]) == thr;
-        }
-        for (int o = 32; o; o >>= 1) eq += __shfl_xor(eq, o);
-        __syncthreads();
-        if (lane == 0) scratch[w] = eq;
-        __syncthreads();
-        for (int i = 0; i < w; ++i) eq_before += scratch[i];
-        __syncthreads();
-    }
-    // a vector's kept weights, whole numbers; e0: equal keys before it in the row
-    const auto kept = [&](int i, u64 e0, u64 out[N], float ws[N]) {
-        float x[N];
-        row.load(i, x);
+    // a vector's kept weights, whole numbers, and their sum
+    const auto kept = [&](int f, const float x[N], u64 out[N], float ws[N]) {
         u64 sum = 0;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const unsigned k = logit_key(x[e]);
-            const int f = row.first(i) + e;
-            bool in = f >= 0 && f < p.vocab && k >= thr;
-            if (k == thr) in = in && e0++ < need;
-            ws[e] = in ? wt.weight(x[e]) : 0.f;
-            if (!(ws[e] >= wt.min_w)) ws[e] = 0.f;
+            ws[e] = wt.weight(x[e]);
+            if (!(ws[e] >= min_w) || (cuts && !s.in(s.within, f + e, logit_key(x[e])))) ws[e] = 0.f;
             out[e] = wt.fixed(ws[e]);
             sum += out[e];
         }
         return sum;
     };
-    const auto equals = [&](int i) {
-        float x[N];
-        row.load(i, x);
-        u64 n = 0;
+    // the least logit that may be kept
+    // (of min_p with more than the rounding of a weight to spare)
+    float least = cuts ? key_logit(s.within.key) : -__builtin_inff();
+    if (min_w > 0.f) least = fmaxf(least, wt.top + (__logf(min_w) - 0.01f) * t * 1.0001f - 1e-30f);
+    const auto none = [&](const float x[N]) {
+        float m = x[0];
 #pragma unroll
-        for (int e = 0; e < N; ++e) n += logit_key(x[e]) == thr;
-        return n;
+        for (int e = 1; e < N; ++e) m = fmaxf(m, x[e]);
+        return m < least;
     };
-    u64 total = 0, e_run = eq_before;
-    for (int i = v0; i < v1; i += 64) {
-        const int v = i + lane;
-        u64 e0 = 0;
-        if (need != ~0ull) {
-            const u64 n = v < v1 ? equals(v) : 0, incl = wave_incl(n);
-            e0 = e_run + incl - n;
-            e_run += __shfl(incl, 63);
-        }
-        u64 out[N];
-        float ws[N];
-        if (v < v1) total += kept(v, e0, out, ws);
+    u64 total = 0;
+    if (cuts || min_w > 0.f) {
+        s.each([&](int f, const float x[N]) {
+            if (none(x)) return;
+            u64 out[N];
+            float ws[N];
+            total += kept(f, x, out, ws);
+        });
+    } else {
+        s.each([&](int, const float x[N]) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) total += wt.biased(wt.weight(x[e]));
+            total -= u64(N) * wt.magic_bits;
+        });
     }
     for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
     __syncthreads();
-    if (lane == 0) scratch[w] = total;
+    if (lane == 0) sh.scratch[w] = total;
     __syncthreads();
     u64 W = 0, lower = 0;
     for (int i = 0; i < kWaves; ++i) {
-        if (i < w) lower += scratch[i];
-        W += scratch[i];
+        if (i < w) lower += sh.scratch[i];
+        W += sh.scratch[i];
     }
     const double target = double(fmaxf(p.u[b], 0.f)) * double(W);
     // the stretch that the target falls in finds the token; u of 1 and more ends at the last kept one
     const bool here = total && !(double(lower) > target) && (double(lower + total) > target || lower + total == W);
     if (!here) return;
     u64 run = lower;
-    e_run = eq_before;
-    int token = -1;
-    float weight = 0.f;
     for (int i = v0; i < v1; i += 64) {
         const int v = i + lane;
-        u64 e0 = 0;
-        if (need != ~0ull) {
-            const u64 n = v < v1 ? equals(v) : 0, incl = wave_incl(n);
-            e0 = e_run + incl - n;
-            e_run += __shfl(incl, 63);
-        }
-        u64 out[N];
+        u64 out[N], mine = 0;
         float ws[N];
-        const u64 mine = v < v1 ? kept(v, e0, out, ws) : 0;
-        const u64 incl = wave_incl(mine), all = __shfl(incl, 63);
-        const u64 m = run + incl - mine;
-        const bool hit = mine && double(m + mine) > target;
-        const u64 who = __ballot(hit);
-        if (who || run + all == W) {
+        if (v < v1) {
+            float x[N];
+            row.load(v, x);
+            if (!none(x)) mine = kept(row.first(v), x, out, ws);
+        }
+        if (!__any(mine != 0)) continue;
+        const u64 incl = wave_incl(mine), sum = __shfl(incl, 63), m = run + incl - mine;
+        const u64 who = __ballot(mine && double(m + mine) > target);
+        if (who || run + sum == W) {
             // past the last sum that exceeds the target, only u >= 1 gets here: the last lane with any weight
             const u64 any = __ballot(mine != 0);
-            const int l = who ? __ffsll((long long)(who)) - 1 : 63 - __clzll((long long)(any));
-            if (lane == l) {
-                u64 s = m;
+            if (lane == (who ? __ffsll((long long)(who)) - 1 : 63 - __clzll((long long)(any)))) {
+                u64 c = m;
+                int token = -1;
+                float weight = 0.f;
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    if (!out[e]) continue;
-                    if (token >= 0 && double(s) > target) continue;
-                    s += out[e];
+                    if (!out[e] || (token >= 0 && double(c) > target)) continue;
+                    c += out[e];
                     token = row.first(v) + e;
                     weight = ws[e];
                 }
@@ -345,14 +582,19 @@ __global__ __launch_bounds__(kThreads) void k_sample(const SampleP p)
             }
             break;
         }
-        run += all;
+        run += sum;
     }
 }
 
 template <class E>
 static void launch_sample(const SampleP& p, uint32_t rows, hipStream_t stream)
 {
-    hipLaunchKernelGGL(k_sample<E>, dim3(rows), dim3(kThreads), 0, stream, p);
+// With a row or less a compute unit, all its waves take one; else half of them, so that two rows' passes and steps between
+    // them overlap.
+    if (rows <= 256)
+        hipLaunchKernelGGL((k_sample<E, 16>), dim3(rows), dim3(1024), 0, stream, p);
+    else
+        hipLaunchKernelGGL((k_sample<E, 8>), dim3(rows), dim3(512), 0, stream, p);
 }
 
 }  // namespace ops
