@@ -174,10 +174,10 @@ struct SlotView {
     {
         int id;
         const size_t at = index(slot, id);
-        if (unsigned(id) >= p.pool.n_blocks) return 0u;
-        const int ps = p.pos[at];
-        if ((long long)(ps) < p.sink || ps >= from) return 0xffffffffu;
-        return score_key(p.score[at]);
+        const bool ok = unsigned(id) < p.pool.n_blocks;
+        const int ps = p.pos[ok ? at : 0];
+        const float sc = p.score[ok ? at : 0];
+        return !ok ? 0u : (long long)(ps) < p.sink || ps >= from ? 0xffffffffu : score_key(sc);
     }
 };
 
@@ -205,43 +205,75 @@ __device__ __forceinline__ int scan16(int v, int& total, int* scratch)
 // One workgroup finds which slots of a request and head stay, by a radix
 // selection of the budget-th largest key in digits of 11, 11 and 10 bits, and
 // lists the moves in slot order: waves own consecutive stretches of slots and
-// count before they write, so that no order is left to chance.
-__global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictP p)
+// count before they write, so that no order is left to chance.  Every pass
+// needs every key: `held` of them (all, up to 32768) are read once and kept in
+// LDS, further ones are read again.  Read in every pass, the longest of 64
+// requests (20000 slots) took 94 us, most of it the latency of three loads that
+// depend on each other.
+constexpr int kHeld = 32768;
+
+__global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictP p, const int held)
 {
+    extern __shared__ unsigned keys[];
     __shared__ int hist[2048];
     __shared__ int scratch[kSelectWaves];
     __shared__ int cut[2];
     __shared__ int wave_a[kSelectWaves], wave_b[kSelectWaves];
-    const int hk = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int hk = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
     const int L = request_len(p.pool, p.batch, r), B = p.budget;
     const SlotView v{p, r, hk, (long long)(p.next_pos[r]) - p.recent};
     if (hk == 0 && tid == 0) p.lens_out[r] = L < B ? L : B;
-    const bool copy = p.score_out != p.score || p.pos_out != p.pos;
+    // what the budget covers goes to the outputs as it is; what moves overwrites the given up places later
+    if (p.score_out != p.score || p.pos_out != p.pos)
+        for (int s = tid; s < min(L, B); s += kSelectThreads) {
+            int id;
+            const size_t at = v.index(s, id);
+            if (unsigned(id) >= p.pool.n_blocks) continue;
+            p.score_out[at] = p.score[at];
+            p.pos_out[at] = p.pos[at];
+        }
     if (L <= B) {
         if (tid == 0) p.n_moves[size_t(r) * p.pool.kv_heads + hk] = 0;
-        if (copy)
-            for (int s = tid; s < L; s += kSelectThreads) {
-                int id;
-                const size_t at = v.index(s, id);
-                if (unsigned(id) >= p.pool.n_blocks) continue;
-                p.score_out[at] = p.score[at];
-                p.pos_out[at] = p.pos[at];
-            }
         return;
     }
+    // a wave reads and writes its own stretch's keys only
+    const int seg = ((L + kSelectThreads - 1) / kSelectThreads) * 64;
+    const int s0 = min(w * seg, L), s1 = min(s0 + seg, L), s2 = min(s1, held);
+    for (int s = s0 + lane; s < s2; s += 256) {
+        unsigned k[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[i] = v.key(min(s + 64 * i, L - 1));
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (s + 64 * i < s2) keys[s + 64 * i] = k[i];
+    }
+    lds_order();
+    // f(slot, whether it is one, its key) for the wave's slots, 64 at a time in slot order
+    const auto each = [&](auto f) {
+        int s = s0 + lane;
+        for (; s - lane + 256 <= s2; s += 256) {
+            unsigned k[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) k[i] = keys[s + 64 * i];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f(s + 64 * i, true, k[i]);
+        }
+        for (; s - lane < s1; s += 64) f(s, s < s1, s < s2 ? keys[s] : s < s1 ? v.key(s) : 0u);
+    };
+
     // thr: the key of rank B; need: how many slots of that key stay, the lowest ones
     unsigned thr = 0, mask = 0;
     int need = B;
     const int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
+#pragma unroll 1
     for (int d = 0; d < 3; ++d) {
-        const int n = 1 << bits[d];
+        const int n = 1 << bits[d], shift = shifts[d];
         hist[tid] = 0;
         hist[tid + 1024] = 0;
         __syncthreads();
-        for (int s = tid; s < L; s += kSelectThreads) {
-            const unsigned k = v.key(s);
-            if ((k & mask) == thr) atomicAdd(&hist[(k >> shifts[d]) & (n - 1)], 1);
-        }
+        each([&](int, bool in, unsigned k) {
+            if (in && (k & mask) == thr) atomicAdd(&hist[(k >> shift) & (n - 1)], 1);
+        });
         __syncthreads();
         // from the largest digit down: thread t takes bins n-1-2t and n-2-2t
         const int hi = n - 1 - 2 * tid, lo = hi - 1;
@@ -251,53 +283,40 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictP p)
         if (above < need && need <= above + a) cut[0] = hi, cut[1] = need - above;
         if (above + a < need && need <= above + a + b) cut[0] = lo, cut[1] = need - above - a;
         __syncthreads();
-        thr |= unsigned(cut[0]) << shifts[d];
-        mask |= unsigned(n - 1) << shifts[d];
+        thr |= unsigned(cut[0]) << shift;
+        mask |= unsigned(n - 1) << shift;
         need = cut[1];
         __syncthreads();
     }
-    // consecutive stretches of slots for the waves
-    const int seg = ((L + kSelectWaves * 64 - 1) / (kSelectWaves * 64)) * 64;
-    const int s0 = w * seg < L ? w * seg : L, s1 = s0 + seg < L ? s0 + seg : L;
     int eq = 0;
-    for (int s = s0 + lane; s - lane < s1; s += 64) {
-        const bool e = s < s1 && v.key(s) == thr;
-        eq += __popcll(__ballot(e));
-    }
+    each([&](int, bool in, unsigned k) { eq += __popcll(__ballot(in && k == thr)); });
     if (lane == 0) wave_a[w] = eq;
     __syncthreads();
     int eq0 = 0;
     for (int i = 0; i < w; ++i) eq0 += wave_a[i];
     __syncthreads();
-    int holes = 0, comers = 0;
+    // how many holes and how many that come the waves before have; then they are written
     const unsigned long long lt = (1ull << lane) - 1;
+    int* const src = p.src + (size_t(r) * p.pool.kv_heads + hk) * p.cap;
+    int* const dst = p.dst + (size_t(r) * p.pool.kv_heads + hk) * p.cap;
+    int holes = 0, comers = 0;
+#pragma unroll 1
     for (int pass = 0; pass < 2; ++pass) {
         int e0 = eq0;
-        int* src = p.src + (size_t(r) * p.pool.kv_heads + hk) * p.cap;
-        int* dst = p.dst + (size_t(r) * p.pool.kv_heads + hk) * p.cap;
-        for (int s = s0 + lane; s - lane < s1; s += 64) {
-            const bool in = s < s1;
-            const unsigned k = in ? v.key(s) : 0u;
+        each([&](int s, bool in, unsigned k) {
             const bool e = in && k == thr;
             const unsigned long long em = __ballot(e);
             const bool keep = in && (k > thr || (e && e0 + __popcll(em & lt) < need));
             e0 += __popcll(em);
-            const unsigned long long hm = __ballot(in && s < B && !keep), cm = __ballot(in && s >= B && keep);
+            const bool hole = in && s < B && !keep, comes = in && s >= B && keep;
+            const unsigned long long hm = __ballot(hole), cm = __ballot(comes);
             if (pass) {
-                if (in && s < B && !keep) dst[holes + __popcll(hm & lt)] = s;
-                if (in && s >= B && keep) src[comers + __popcll(cm & lt)] = s;
-                if (copy && s < B && keep) {
-                    int id;
-                    const size_t at = v.index(s, id);
-                    if (unsigned(id) < p.pool.n_blocks) {
-                        p.score_out[at] = p.score[at];
-                        p.pos_out[at] = p.pos[at];
-                    }
-                }
+                if (hole) dst[holes + __popcll(hm & lt)] = s;
+                if (comes) src[comers + __popcll(cm & lt)] = s;
             }
             holes += __popcll(hm);
             comers += __popcll(cm);
-        }
+        });
         if (pass) break;
         if (lane == 0) wave_a[w] = holes, wave_b[w] = comers;
         __syncthreads();
@@ -326,23 +345,37 @@ __global__ __launch_bounds__(256) void k_evict_move(const EvictP p, const int pi
     const int* dst = p.dst + at * p.cap + m0;
     const int omask = (1 << p.pool.lb) - 1;
     const int32_t* table = p.batch.table + size_t(r) * p.batch.width;
-    for (int u = threadIdx.x; u < rows * pieces; u += 256) {
-        const int m = u / pieces, d = u % pieces * 16;
-        const int a = src[m], b = dst[m];
-        const int ia = table[a >> p.pool.lb], ib = table[b >> p.pool.lb];
-        if (unsigned(ia) >= p.pool.n_blocks || unsigned(ib) >= p.pool.n_blocks) continue;
-        const int oa = a & omask, ob = b & omask;
-        const char* kh = head_of(p.pool.k, p.pool.k_head, hk);
-        const char* vh = head_of(p.pool.v, p.pool.v_head, hk);
-        *reinterpret_cast<u32x4*>(const_cast<char*>(row_of(kh, p.pool.k_block, p.pool.k_token, ib, ob)) + d) =
-            *reinterpret_cast<const u32x4*>(row_of(kh, p.pool.k_block, p.pool.k_token, ia, oa) + d);
-        *reinterpret_cast<u32x4*>(const_cast<char*>(row_of(vh, p.pool.v_block, p.pool.v_token, ib, ob)) + d) =
-            *reinterpret_cast<const u32x4*>(row_of(vh, p.pool.v_block, p.pool.v_token, ia, oa) + d);
-        if (d == 0) {
-            const size_t sa = ((size_t(ia) * p.pool.kv_heads + hk) << p.pool.lb) + oa, sb = ((size_t(ib) * p.pool.kv_heads + hk) << p.pool.lb) + ob;
-            p.score_out[sb] = p.score[sa];
-            p.pos_out[sb] = p.pos[sa];
+    const char* kh = head_of(p.pool.k, p.pool.k_head, hk);
+    const char* vh = head_of(p.pool.v, p.pool.v_head, hk);
+    constexpr int U = 4;
+    for (int u0 = threadIdx.x; u0 < rows * pieces; u0 += 256 * U) {
+        // sources are no destinations: all loads first
+        u32x4 k[U], v[U];
+        char *kt[U], *vt[U];
+#pragma unroll
+        for (int i = 0; i < U; ++i) {
+            const int u = u0 + 256 * i, m = u / pieces, d = u % pieces * 16;
+            kt[i] = nullptr;
+            if (u >= rows * pieces) continue;
+            const int a = src[m], b = dst[m], oa = a & omask, ob = b & omask;
+            const int ia = table[a >> p.pool.lb], ib = table[b >> p.pool.lb];
+            if (unsigned(ia) >= p.pool.n_blocks || unsigned(ib) >= p.pool.n_blocks) continue;
+            k[i] = *reinterpret_cast<const u32x4*>(row_of(kh, p.pool.k_block, p.pool.k_token, ia, oa) + d);
+            v[i] = *reinterpret_cast<const u32x4*>(row_of(vh, p.pool.v_block, p.pool.v_token, ia, oa) + d);
+            kt[i] = const_cast<char*>(row_of(kh, p.pool.k_block, p.pool.k_token, ib, ob)) + d;
+            vt[i] = const_cast<char*>(row_of(vh, p.pool.v_block, p.pool.v_token, ib, ob)) + d;
+            if (d == 0) {
+                const size_t sa = ((size_t(ia) * p.pool.kv_heads + hk) << p.pool.lb) + oa, sb = ((size_t(ib) * p.pool.kv_heads + hk) << p.pool.lb) + ob;
+                p.score_out[sb] = p.score[sa];
+                p.pos_out[sb] = p.pos[sa];
+            }
         }
+#pragma unroll
+        for (int i = 0; i < U; ++i)
+            if (kt[i]) {
+                *reinterpret_cast<u32x4*>(kt[i]) = k[i];
+                *reinterpret_cast<u32x4*>(vt[i]) = v[i];
+            }
     }
 }
 
@@ -463,7 +496,12 @@ int mts_evict(const mts_evict_args* a, hipStream_t stream)
     p.n_moves = reinterpret_cast<int*>(ws);
     p.src = reinterpret_cast<int*>(ws + s.src);
     p.dst = reinterpret_cast<int*>(ws + s.dst);
-    hipLaunchKernelGGL(k_evict_select, dim3(a->pool.kv_heads, a->batch.n), dim3(kSelectThreads), 0, stream, p);
+    // keys in LDS: what the longest request that the table holds can have
+    static const bool roomy = hipFuncSetAttribute(reinterpret_cast<const void*>(k_evict_select), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                                  4 * kHeld) == hipSuccess;
+    const uint64_t most = uint64_t(a->batch.table_width) * a->pool.block_tokens, room = roomy ? kHeld : 8192;
+    const int held = int(most < room ? most : room);
+    hipLaunchKernelGGL(k_evict_select, dim3(a->pool.kv_heads, a->batch.n), dim3(kSelectThreads), 4 * size_t(held), stream, p, held);
     if (s.cap)
         hipLaunchKernelGGL(k_evict_move, dim3(uint32_t(ceil_div(s.cap, kMoveRows)), uint32_t(rows)), dim3(256), 0, stream, p,
                            int(a->pool.head_dim / 8));
