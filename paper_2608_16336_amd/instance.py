@@ -1,0 +1,266 @@
+"""One serving instance computing what the scheduler accounts for.
+
+The scheduling step counts an instance's KV blocks and its requests' tokens;
+here an instance holds such a pool of blocks in earnest and runs a small
+random-weight attention layer over it, tick by tick, on the operators of
+:mod:`paper_2608_16336_amd.ops`:
+
+    rotary positions and the append to the blocks (rope_append), attention of
+    every request's token or drafted tree over them (attend), the weights its
+    slots receive (weigh), the draw of the next tokens (sample), and, when the
+    pool runs out of blocks, the eviction of the least attended slots (evict)
+    where the scheduler would preempt.
+
+The command takes a cluster that the scheduler has run for a while, fills an
+instance with the running requests of one of its instances and decodes:
+
+    python -m paper_2608_16336_amd.instance --preset tiny --ticks 32 --branches 2 --depth 3
+"""
+import argparse
+import os
+import sys
+
+import torch
+
+from . import ops
+
+
+class Instance:
+    """A pool of `blocks` KV blocks and one attention layer of random weights.
+
+    Requests come with their prompt tokens (``admit``); ``tick`` lets every
+    request emit one token, or more where drafted ones are confirmed.  Drafts
+    come from the layer without its attention: `branches` first guesses, each
+    followed by the greedy chain of `depth` tokens.  `budget` slots a request
+    are kept when blocks run out, among them the last `recent` positions."""
+
+    def __init__(self, blocks, block_tokens=16, q_heads=8, kv_heads=2, head_dim=64, vocab=1024, dtype=torch.bfloat16, branches=0, depth=1,
+                 temperature=0.0, top_k=0, top_p=1.0, min_p=0.0, budget=None, recent=32, sink=4, decay=1.0, seed=0, device="cuda"):
+        g = torch.Generator().manual_seed(seed)
+        r = lambda *s: torch.randn(*s, generator=g)  # noqa: E731
+        self.bt, self.Hq, self.Hkv, self.D, self.vocab = block_tokens, q_heads, kv_heads, head_dim, vocab
+        width = q_heads * head_dim
+        self.embed = r(vocab, width).to(device, dtype)
+        self.wqkv = (r((q_heads + 2 * kv_heads) * head_dim, width) * width ** -0.5).to(device, dtype)
+        self.wo = (r(width, width) * width ** -0.5).to(device, dtype)
+        shape = (blocks, kv_heads, block_tokens, head_dim)
+        self.k = torch.empty(shape, dtype=dtype, device=device)
+        self.v = torch.empty_like(self.k)
+        self.score = torch.zeros(shape[:3], device=device)
+        self.pos = torch.zeros(shape[:3], dtype=torch.int32, device=device)
+        self.freqs = ops.rope_freqs(head_dim, device=device)
+        self.free = list(range(blocks))[::-1]
+        self.requests = []  # dict(blocks, len, next_pos, tokens): slots in use, position of the next token, all tokens so far
+        self.branches, self.depth = branches, depth
+        self.rule = (temperature, top_k, top_p, min_p)
+        self.budget, self.recent, self.sink, self.decay = budget, recent, sink, decay
+        self.uniform = torch.Generator().manual_seed(seed + 1)
+        self.device, self.dtype = torch.device(device), dtype
+        self.evictions = 0
+        if branches:
+            self._guess = torch.topk((self.embed.float() @ self.embed.float().t()).fill_diagonal_(-1e30), max(1, branches), dim=1)[1].tolist()
+
+    # ---------------------------------------------------------------- blocks
+
+    def blocks_in_use(self):
+        return sum(len(r["blocks"]) for r in self.requests)
+
+    def _grow(self, r, slots):
+        need = -(-slots // self.bt) - len(r["blocks"])
+        if need > len(self.free):
+            return False
+        for _ in range(need):
+            r["blocks"].append(self.free.pop())
+        return True
+
+    def _shrink(self, r):
+        keep = -(-r["len"] // self.bt)
+        self.free += r["blocks"][keep:]
+        del r["blocks"][keep:]
+
+    def _table(self):
+        width = max(len(r["blocks"]) for r in self.requests)
+        rows = [r["blocks"] + [-1] * (width - len(r["blocks"])) for r in self.requests]
+        return torch.tensor(rows, dtype=torch.int32, device=self.device)
+
+    def _int(self, values):
+        return torch.tensor(values, dtype=torch.int32, device=self.device)
+
+    def evict(self):
+        """Every request shrinks to the budget; its blocks past it are free again."""
+        lens = ops.evict(self.k, self.v, self.score, self.pos, self._table(), self._int([r["len"] for r in self.requests]),
+                         self._int([r["next_pos"] for r in self.requests]), self.budget, recent=self.recent, sink=self.sink).tolist()
+        for r, n in zip(self.requests, lens):
+            r["len"] = n
+            self._shrink(r)
+        self.evictions += 1
+
+    # ---------------------------------------------------------------- the layer
+
+    def _pass(self, requests, tokens, offsets, tree, weigh=True):
+        """The layer for new tokens of some requests (lists of token ids and of position offsets, request by request): their
+        rows go to the slots after each request's own.  Returns the logits of all new tokens."""
+        news = [len(t) for t in tokens]
+        table_rows, self.requests = self.requests, requests
+        table = self._table()
+        self.requests = table_rows
+        start = [0]
+        for n in news:
+            start.append(start[-1] + n)
+        slots, positions = [], []
+        for r, n, off in zip(requests, news, offsets):
+            for i in range(n):
+                s = r["len"] + i
+                slots.append(r["blocks"][s // self.bt] * self.bt + s % self.bt)
+                positions.append(r["next_pos"] + off[i])
+        x = self.embed[torch.tensor([t for row in tokens for t in row], device=self.device)]
+        qkv = x @ self.wqkv.t()
+        q, k, v = (t.view(len(slots), -1, self.D) for t in qkv.split([self.Hq * self.D, self.Hkv * self.D, self.Hkv * self.D], dim=1))
+        q = ops.rope_append(q, k, v, self._int(positions), torch.tensor(slots, dtype=torch.int64, device=self.device), self.freqs,
+                            self.k, self.v, self.pos)
+        lens, q_start = self._int([r["len"] + n for r, n in zip(requests, news)]), self._int(start)
+        out, lse = ops.attend(q, self.k, self.v, table, lens, q_start, max(news), tree=tree)
+        if weigh:
+            ops.weigh(q, lse, self.k, table, lens, q_start, max(news), self.score, decay=self.decay, tree=tree)
+        h = x + out.reshape(len(slots), -1) @ self.wo.t()
+        return h @ self.embed.t()
+
+    def _draw(self, logits):
+        n = logits.shape[0]
+        t, k, p, m = self.rule
+        full = lambda v, dt=torch.float32: torch.full((n,), v, dtype=dt, device=self.device)  # noqa: E731
+        u = torch.rand(n, generator=self.uniform).to(self.device)
+        return ops.sample(logits, u, full(t), full(k, torch.int32), full(p), full(m))[0].tolist()
+
+    # ---------------------------------------------------------------- requests
+
+    def admit(self, prompts):
+        """Requests of these prompts (lists of token ids) join; their prompts but
+        the last token go to the pool in one pass.  Returns False, and takes
+        none, when the blocks do not suffice."""
+        if sum(-(-len(p) // self.bt) for p in prompts) > len(self.free):
+            return False
+        new = []
+        for p in prompts:
+            r = dict(blocks=[], len=0, next_pos=0, tokens=list(p))
+            self._grow(r, len(p))
+            new.append(r)
+        chunks = [p[:-1] for p in prompts]
+        if any(chunks):
+            self._pass(new, chunks, [range(len(c)) for c in chunks], None)
+        for r, c in zip(new, chunks):
+            r["len"] = r["next_pos"] = len(c)
+        self.requests += new
+        return True
+
+    def _draft(self, last):
+        """Tokens, parents and depths of a request's tree below its last token."""
+        tokens, parents, depths = [last], [-1], [0]
+        for first in self._guess[last][:self.branches] if self.branches else []:
+            parent, tok = 0, first
+            for d in range(1, self.depth + 1):
+                tokens.append(tok)
+                parents.append(parent)
+                depths.append(d)
+                parent, tok = len(tokens) - 1, self._guess[tok][0]
+        return tokens, parents, depths
+
+    def tick(self):
+        """Every request emits its next token, and more where its drafts are
+        what the layer draws.  Returns the emitted tokens, request by request."""
+        if not self.requests:
+            return []
+        trees = [self._draft(r["tokens"][-1]) for r in self.requests]
+        most = [len(t[0]) for t in trees]
+        if not all(self._grow(r, r["len"] + n) for r, n in zip(self.requests, most)):
+            if self.budget is None:
+                raise RuntimeError("out of KV blocks")
+            self.evict()
+            if not all(self._grow(r, r["len"] + n) for r, n in zip(self.requests, most)):
+                raise RuntimeError("out of KV blocks: the budget is too large for the pool")
+        bits = None
+        if self.branches:
+            rows, words = [], -(-max(most) // 64)
+            for _, parents, _ in trees:
+                mine = []
+                for i, p in enumerate(parents):
+                    mine.append((mine[p] if p >= 0 else 0) | 1 << i)
+                rows += [[(b >> 64 * w & (1 << 64) - 1) - ((b >> 64 * w + 63 & 1) << 64) for w in range(words)] for b in mine]
+            bits = torch.tensor(rows, dtype=torch.int64, device=self.device)
+        drawn = self._draw(self._pass(self.requests, [t[0] for t in trees], [t[2] for t in trees], bits))
+        emitted, at, moves = [], 0, []
+        for r, (tokens, parents, _) in zip(self.requests, trees):
+            node, path, out = 0, [0], []
+            while True:
+                out.append(drawn[at + node])
+                node = next((i for i in range(1, len(tokens)) if parents[i] == node and tokens[i] == out[-1]), None)
+                if node is None:
+                    break
+                path.append(node)
+            # the confirmed tokens' rows close up behind the request's own
+            moves += [(r, r["len"] + i, r["len"] + n) for i, n in enumerate(path) if i != n]
+            r["len"] += len(path)
+            r["next_pos"] += len(path)
+            r["tokens"] += out
+            emitted.append(out)
+            at += len(tokens)
+        if moves:
+            def where(slots):
+                return (torch.tensor([r["blocks"][s // self.bt] for r, s in slots], device=self.device), slice(None),
+                        torch.tensor([s % self.bt for _, s in slots], device=self.device))
+            to, frm = where([(r, a) for r, a, _ in moves]), where([(r, b) for r, _, b in moves])
+            for x in (self.k, self.v, self.score, self.pos):
+                x[to] = x[frm]
+        for r in self.requests:
+            self._shrink(r)
+        return emitted
+
+
+def main(argv=None):
+    from workloads import preset
+
+    from .mts import Scheduler
+    ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
+    ap.add_argument("--preset", default="tiny")
+    ap.add_argument("--warm", type=int, default=400, help="ticks that the scheduler runs before")
+    ap.add_argument("--instance", type=int, default=0)
+    ap.add_argument("--ticks", type=int, default=32)
+    ap.add_argument("--branches", type=int, default=0, help="drafted branches a request")
+    ap.add_argument("--depth", type=int, default=3, help="drafted tokens a branch")
+    ap.add_argument("--temperature", type=float, default=0.8)
+    ap.add_argument("--top-p", type=float, default=0.95)
+    ap.add_argument("--spare", type=float, default=0.05, help="blocks beyond those in use, as a share; an eviction when they run out")
+    a = ap.parse_args(argv)
+    cfg = preset(a.preset)
+    for g in cfg["groups"]:
+        g["n_replicas"] = 1
+    s = Scheduler(cfg)
+    s.step(a.warm)
+    st = s.export(0, 1)
+    meta = st["meta"].reshape(s.I, s.S)[a.instance]
+    lens = [int(x) & 0xffff for x, m in zip(st["lr"].reshape(s.I, s.S)[a.instance], meta) if m & 3 == 2]
+    used = cfg["kv_blocks"] - int(st["free"][a.instance])
+    s.close()
+    if not lens:
+        print("instance %d runs no request after %d ticks" % (a.instance, a.warm))
+        return
+    g = torch.Generator().manual_seed(1)
+    prompts = [torch.randint(0, 1024, (n,), generator=g).tolist() for n in lens]
+    room = sum(-(-n // cfg["block_tokens"]) for n in lens)
+    inst = Instance(int(room * (1 + a.spare)) + len(lens) * (1 + a.branches * a.depth // cfg["block_tokens"] + 1), cfg["block_tokens"],
+                    branches=a.branches, depth=a.depth, temperature=a.temperature, top_p=a.top_p,
+                    budget=max(64, int(0.75 * sum(lens) / len(lens))))
+    inst.admit(prompts)
+    print("%d running requests, %d tokens in %d blocks of %d (the scheduler counts %d)" % (
+        len(lens), sum(lens), inst.blocks_in_use(), cfg["block_tokens"], used))
+    tokens = 0
+    for _ in range(a.ticks):
+        tokens += sum(len(t) for t in inst.tick())
+    torch.cuda.synchronize()
+    print("%d ticks: %d tokens, %.2f a request and tick; %d evictions; %d blocks in use, %d free" % (
+        a.ticks, tokens, tokens / (a.ticks * len(lens)), inst.evictions, inst.blocks_in_use(), len(inst.free)))
+
+
+if __name__ == "__main__":
+    sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    main()
