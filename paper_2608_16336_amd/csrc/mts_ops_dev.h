@@ -213,16 +213,17 @@ struct Share {
     int r, L, T, first, groups, rounds;
 };
 
+__device__ __forceinline__ Share share_with(const SplitRule& s, int r, int L, int T, int first)
+{
+    return Share{r, L, T, first, s.rows ? int((int64_t(T) * s.G + s.rows - 1) / s.rows) : (T ? 1 : 0), L ? (L + s.unit - 1) / s.unit : 1};
+}
+
 __device__ __forceinline__ Share share_of(const Pool& p, const Batch& b, const SplitRule& s, int r)
 {
-    Share q{r, 0, 0, 0, 0, 1};
-    if (r < b.n) {
-        q.L = request_len(p, b, r);
-        request_tokens(b, r, q.first, q.T);
-        q.groups = s.rows ? int((int64_t(q.T) * s.G + s.rows - 1) / s.rows) : (q.T ? 1 : 0);
-        q.rounds = q.L ? (q.L + s.unit - 1) / s.unit : 1;
-    }
-    return q;
+    int first = 0, T = 0;
+    if (r >= b.n) return share_with(s, r, 0, 0, 0);
+    request_tokens(b, r, first, T);
+    return share_with(s, r, request_len(p, b, r), T, first);
 }
 
 // A value that all lanes have alike, in a scalar register.
@@ -253,19 +254,28 @@ struct Jobs {
     const Batch& b;
     const SplitRule& s;
     int64_t* scratch;  // NW + 4 words of LDS
-    int* order;        // [NT] the thread's request, and how many of a head's jobs come before it: in LDS, not in registers
+    // in LDS, for one request a thread: the requests in order, how many of a head's jobs come before each, and what the
+    // global arrays say of them
+    int* order;        // [NT]
     int64_t* before;   // [NT]
+    int* said;         // [3][NT] slots, new tokens, first new token by request
     int per;
     int64_t head, jobs;  // jobs of a head, of all
 
+    __device__ __forceinline__ Share share(int r) const
+    {
+        return b.n <= NT ? share_with(s, r, said[r], said[NT + r], said[2 * NT + r]) : share_of(p, b, s, r);
+    }
     __device__ __forceinline__ int64_t count(const Share& x) const { return int64_t((x.rounds + per - 1) / per) * x.groups; }
 
     __device__ __forceinline__ Jobs(const Pool& p_, const Batch& b_, const SplitRule& s_, int64_t* scratch_) : p(p_), b(b_), s(s_), scratch(scratch_)
     {
         __shared__ int order_[NT];
         __shared__ int64_t before_[NT];
+        __shared__ int said_[3 * NT];
         order = order_;
         before = before_;
+        said = said_;
         const int t = threadIdx.x;
         Share q{};
         int64_t rounds = 0;
@@ -278,6 +288,9 @@ struct Jobs {
         if (b.n <= NT) {
             int* len = reinterpret_cast<int*>(before);
             len[t] = q.rounds;
+            said[t] = q.L;
+            said[NT + t] = q.T;
+            said[2 * NT + t] = q.first;
             __syncthreads();
             if (t < b.n) {
                 int rank = 0;
@@ -285,7 +298,7 @@ struct Jobs {
                 order[rank] = t;
             }
             __syncthreads();
-            if (t < b.n) q = share_of(p, b, s, order[t]);
+            if (t < b.n) q = share(order[t]);
             head = uniform(prefix(count(q), 0));
         } else {
             int64_t n = 0;
@@ -341,7 +354,7 @@ struct Jobs {
             __syncthreads();
             if (in < end) break;
         }
-        const Share q = share_of(p, b, s, uniform(found[0]));
+        const Share q = share(uniform(found[0]));
         const int i = uniform(found[1]), rounds = uniform(q.rounds);
         j.id = int(id);
         j.hk = hk;
