@@ -36,26 +36,44 @@ struct Row {
     }
     // index of element 0 of vector i
     __device__ __forceinline__ int first(int i) const { return i * N - skip; }
+    // (an aligned vector with an element of the row in it lies in one piece of memory with it and can be read whole)
     __device__ __forceinline__ V raw(int i) const
     {
-        const int f = first(i);
-        if (f >= 0 && f + N <= vocab) return *reinterpret_cast<const V*>(start + 16 * size_t(i));
-        V v;
-#pragma unroll
-        for (int e = 0; e < N; ++e)
-            v.e[e] = f + e >= 0 && f + e < vocab ? *reinterpret_cast<const E*>(start + 16 * size_t(i) + e * sizeof(E)) : E(-__builtin_inff());
-        return v;
+        return *reinterpret_cast<const V*>(start + 16 * size_t(i));
     }
     // NaN as -inf
-    __device__ __forceinline__ void widen(const V& v, float x[N]) const
+    static __device__ __forceinline__ float widen(E e)
     {
+        const float f = float(e);
+        return f != f ? -__builtin_inff() : f;
+    }
+    // f(index of the first one, four elements) for the vector's elements in turn: the code of the passes stays half as
+    // large as with eight 16-bit elements side by side
+    template <class F>
+    __device__ __forceinline__ void fours(int i, const V& v, F f) const
+    {
+        struct alignas(8) Four {
+            E e[4];
+        };
+        struct Parts {
+            Four p[N / 4];
+        };
+        const Parts parts = __builtin_bit_cast(Parts, v);
+        Four now = parts.p[0];
+#pragma unroll 1
+        for (int h = 0; h < N / 4; ++h) {
+            float x[4];
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float f = float(v.e[e]);
-            x[e] = f != f ? -__builtin_inff() : f;
+            for (int e = 0; e < 4; ++e) x[e] = widen(now.e[e]);
+            const int at = first(i) + 4 * h;
+            if (at < 0 || at + 4 > vocab) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) x[e] = unsigned(at + e) < unsigned(vocab) ? x[e] : -__builtin_inff();
+            }
+            f(at, x);
+            now = parts.p[N / 4 - 1];
         }
     }
-    __device__ __forceinline__ void load(int i, float x[N]) const { widen(raw(i), x); }
 };
 
 __device__ __forceinline__ unsigned logit_key(float x)
@@ -80,11 +98,14 @@ struct Weigher {
     __device__ __forceinline__ u64 fixed(float w) const { return biased(w) - magic_bits; }
 };
 
+__device__ __forceinline__ float uniform_f(float x) { return __uint_as_float(unsigned(uniform(int(__float_as_uint(x))))); }
+__device__ __forceinline__ u64 uniform_u(u64 x) { return u64(uniform(int64_t(x))); }
+
 // Sum over the lower threads of a workgroup, and the total.
 template <int kWaves>
 __device__ __forceinline__ u64 block_before(u64 v, u64& total, u64* scratch)
 {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, w = uniform(int(threadIdx.x >> 6));
     u64 incl = v;
     for (int o = 1; o < 64; o <<= 1) {
         const u64 u = __shfl_up(incl, o);
@@ -95,10 +116,12 @@ __device__ __forceinline__ u64 block_before(u64 v, u64& total, u64* scratch)
     __syncthreads();
     u64 before = incl - v;
     total = 0;
+#pragma unroll 4
     for (int i = 0; i < kWaves; ++i) {
         if (i < w) before += scratch[i];
         total += scratch[i];
     }
+    total = uniform_u(total);
     return before;
 }
 
@@ -125,11 +148,11 @@ struct Cut {
 
 template <class E, int kWaves>
 struct Sampler {
-    static constexpr int N = Row<E>::N, kThreads = 64 * kWaves, kEach = kBins / kThreads;  // bins a thread
+    static constexpr int N = 4, kThreads = 64 * kWaves, kEach = kBins / kThreads;  // elements at a time, bins a thread
     struct Shared {
         u64 sum[kBins];
-        u64 c_order[kCandidates], c_share[kCandidates];  // see order(); what the rule sums
-        u64 r_order[kCandidates], r_share[kCandidates];  // the same by rank
+        u64 c_order[kCandidates];                        // see order()
+        u64 r_order[kCandidates], r_share[kCandidates];  // the same by rank, and what the rule sums
         u64 scratch[kWaves];
         u64 above;
         unsigned lo, hi;
@@ -141,24 +164,28 @@ struct Sampler {
     int v0, v1;  // the wave's vectors: consecutive, so that waves, vectors and lanes are in vocabulary order
     Cut within;  // what rules before this one have kept
 
-    // f(index of the vector's element 0, its elements) for the wave's vectors, with three loads on their way
+    // f(index of the first one, four elements) for vectors of [from, to), 64 in turn, with three loads on their way
+    template <class F>
+    __device__ __forceinline__ void each(int from, int to, F f) const
+    {
+        typename Row<E>::V a{}, b{}, c{};
+        const int i0 = from + int(threadIdx.x & 63);
+        if (i0 < to) a = row.raw(i0);
+        if (i0 + 64 < to) b = row.raw(i0 + 64);
+        if (i0 + 128 < to) c = row.raw(i0 + 128);
+#pragma unroll 1
+        for (int i = i0; i < to; i += 64) {
+            const typename Row<E>::V now = a;
+            a = b;
+            b = c;
+            if (i + 192 < to) c = row.raw(i + 192);
+            row.fours(i, now, f);
+        }
+    }
     template <class F>
     __device__ __forceinline__ void each(F f) const
     {
-        typename Row<E>::V a{}, b{}, c{};
-        const int i0 = v0 + int(threadIdx.x & 63);
-        if (i0 < v1) a = row.raw(i0);
-        if (i0 + 64 < v1) b = row.raw(i0 + 64);
-        if (i0 + 128 < v1) c = row.raw(i0 + 128);
-#pragma unroll 1
-        for (int i = i0; i < v1; i += 64) {
-            float x[N];
-            row.widen(a, x);
-            a = b;
-            b = c;
-            if (i + 192 < v1) c = row.raw(i + 192);
-            f(row.first(i), x);
-        }
+        each(v0, v1, f);
     }
     __device__ __forceinline__ bool in(const Cut& c, int index, unsigned k) const { return k > c.key || (k == c.key && index <= c.index); }
 
@@ -181,7 +208,7 @@ struct Sampler {
     static __device__ __forceinline__ int order_index(u64 o) { return 0x7fffffff - int(unsigned(o)); }
 
     // The listed tokens by rank; returns how many there are.
-    __device__ __forceinline__ int rank_listed()
+    __device__ __forceinline__ int rank_listed(bool by_mass)
     {
         const int n = sh.n, t = threadIdx.x;
         if (t < n) {
@@ -189,7 +216,7 @@ struct Sampler {
             int rank = 0;
             for (int i = 0; i < n; ++i) rank += sh.c_order[i] > mine;
             sh.r_order[rank] = mine;
-            sh.r_share[rank] = sh.c_share[t];
+            sh.r_share[rank] = share(by_mass, key_logit(order_key(mine)));
         }
         __syncthreads();
         return n;
@@ -212,7 +239,7 @@ struct Sampler {
             before += x[i];
         }
         __syncthreads();
-        const int bin = sh.bin;
+        const int bin = uniform(sh.bin);
 #pragma unroll
         for (int i = kEach - 1; i >= 0; --i) {
             before -= x[i];
@@ -224,13 +251,19 @@ struct Sampler {
     // The last rank kept, ranks being kept while the sum before them (of ranks, or of weights) is below the limit.  The
     // bins of the whole row are filled; where more tokens share the cut's bin than can be ranked one by one, it is divided
     // by keys, 2048 ways at a time.
-    __device__ __forceinline__ Cut find(bool by_mass, double limit)
+    //
+    // The pass that lists the cut's bin also sums, for this thread, the weights of what lies above it (of at least min_w);
+    // `listed` says whether that bin's tokens are all listed, so that with those of them that are kept these are all the
+    // kept weights.
+    __device__ __forceinline__ Cut find(bool by_mass, double limit, float min_w, u64& sure, bool& listed)
     {
+        sure = 0;
+        listed = true;
         __syncthreads();
         if (threadIdx.x == 0) sh.above = 0;
         __syncthreads();
         find_bin(limit);
-        const float bin = float(sh.bin), next = sh.bin == kBins - 1 ? __builtin_inff() : bin + 1.f;
+        const float bin = uniform_f(float(sh.bin)), next = bin == float(kBins - 1) ? __builtin_inff() : bin + 1.f;
         unsigned lo = 0, hi = 0xffffffffu;  // what is left: this bin's tokens whose keys lie between
         const auto left = [&](int index, float x, unsigned k) {
             const float d = bins_down(x);
@@ -242,11 +275,20 @@ struct Sampler {
             __syncthreads();
             unsigned least = 0xffffffffu, most = 0;
             each([&](int f, const float x[N]) {
-                unsigned some = 0;
+                unsigned some = 0, over = 0;
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
                     const float d = bins_down(x[e]);
+                    over |= unsigned(d < bin) << e;
                     some |= unsigned(d >= bin && d < next) << e;
+                }
+                if (listed && over) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) {
+                        const float w = wt.weight(x[e]);
+                        const bool counts = ((over >> e) & 1) && w >= min_w && in(within, f + e, logit_key(x[e]));
+                        sure += wt.fixed(counts ? w : 0.f);
+                    }
                 }
                 if (!some) return;
 #pragma unroll
@@ -257,16 +299,15 @@ struct Sampler {
                     least = min(least, k);
                     most = max(most, k);
                     const int at = atomicAdd(&sh.n, 1);
-                    if (at >= kCandidates) continue;
-                    sh.c_order[at] = order(k, f + e);
-                    sh.c_share[at] = share(by_mass, x[e]);
+                    if (at < kCandidates) sh.c_order[at] = order(k, f + e);
                 }
             });
             if (most >= least) atomicMin(&sh.lo, least), atomicMax(&sh.hi, most);
             __syncthreads();
             if (sh.n <= kCandidates) break;
-            lo = sh.lo;
-            hi = sh.hi;
+            listed = false;
+            lo = unsigned(uniform(int(sh.lo)));
+            hi = unsigned(uniform(int(sh.hi)));
             if (lo == hi) return find_equal(by_mass, limit, lo);
             const int shift = max(0, 32 - __clz(int(hi - lo)) - 11);
             clear();
@@ -279,73 +320,54 @@ struct Sampler {
             });
             __syncthreads();
             find_bin(limit);
-            hi -= unsigned(sh.bin) << shift;
+            hi -= unsigned(uniform(sh.bin)) << shift;
             const unsigned width = (1u << shift) - 1;
             lo = hi - lo > width ? hi - width : lo;
         }
-        const int n = rank_listed(), t = threadIdx.x;
+        const int n = uniform(rank_listed(by_mass)), t = threadIdx.x;
         u64 total;
         const u64 above = sh.above, before = above + block_before<kWaves>(t < n ? sh.r_share[t] : 0, total, sh.scratch);
         if (t < n && begins(before, limit)) atomicMax(&sh.best, t);
         __syncthreads();
         const u64 last = sh.r_order[sh.best];
         __syncthreads();
-        return Cut{order_key(last), order_index(last)};
+        return Cut{unsigned(uniform(int(order_key(last)))), uniform(order_index(last))};
     }
 
-    // Where the kept tokens are few they are found without bins of the whole row, and the token is drawn from their list.
+    // The k first ranks of a small k are found without bins of the whole row, and the token is drawn from their list.
     // `most` is the largest logit that this thread has met: as many of the threads' largest as there are ranks wanted are
-    // at or above some bin, hence at least so many tokens are, and seldom many more.  They are listed in one pass, with
-    // the sum of all weights where top-p asks for it.  Returns false if they do not fit or do not reach the share that
-    // top-p keeps.
-    __device__ __forceinline__ bool draw_few(float most, int k, float top_p, float min_w, float u, int frac, int32_t* token, float* logprob)
+    // at or above some bin, hence at least so many tokens are, and seldom many more.  They are listed in one pass.  Returns
+    // false if they do not fit.
+    __device__ __forceinline__ bool draw_few(float most, int k, float top_p, float min_w, const SampleP& p)
     {
-        const bool by_p = top_p < 1.f;
         const int t = threadIdx.x;
         clear();
         if (t == 0) sh.above = 0, sh.n = 0, sh.best = -1;
         atomicAdd(&sh.sum[int(bins_down(most))], 1ull);
         __syncthreads();
-        find_bin(double(k ? k : kFew - 64));
-        const float next = sh.bin == kBins - 1 ? __builtin_inff() : float(sh.bin + 1);
-        u64 z = 0;
+        find_bin(double(k));
+        const float next = uniform_f(sh.bin == kBins - 1 ? __builtin_inff() : float(sh.bin + 1));
         each([&](int f, const float x[N]) {
             float m = x[0];
 #pragma unroll
             for (int e = 1; e < N; ++e) m = fmaxf(m, x[e]);
-            if (bins_down(m) < next) {
+            if (!(bins_down(m) < next)) return;
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    // (what lies outside the row reads as -inf and would be listed for it)
-                    if (!(bins_down(x[e]) < next) || unsigned(f + e) >= unsigned(row.vocab)) continue;
-                    const int at = atomicAdd(&sh.n, 1);
-                    if (at >= kCandidates) continue;
-                    sh.c_order[at] = order(logit_key(x[e]), f + e);
-                    sh.c_share[at] = wt.fixed(wt.weight(x[e]));
-                }
-            }
-            if (by_p && !k) {
-#pragma unroll
-                for (int e = 0; e < N; ++e) z += wt.biased(wt.weight(x[e]));
-                z -= u64(N) * wt.magic_bits;
+            for (int e = 0; e < N; ++e) {
+                // (what lies outside the row reads as -inf and would be listed for it)
+                if (!(bins_down(x[e]) < next) || unsigned(f + e) >= unsigned(row.vocab)) continue;
+                const int at = atomicAdd(&sh.n, 1);
+                if (at < kCandidates) sh.c_order[at] = order(logit_key(x[e]), f + e);
             }
         });
         __syncthreads();
         if (sh.n > kCandidates) return false;
-        const int n = rank_listed();
-        u64 total, all, W;
-        const u64 share = t < n && (!k || t < k) ? sh.r_share[t] : 0;
+        const int n = uniform(rank_listed(true));
+        u64 total, W;
+        const bool ranked = t < n && t < k;
+        const u64 share = ranked ? sh.r_share[t] : 0;
         const u64 before = block_before<kWaves>(share, total, sh.scratch);
-        bool keep = t < n && (!k || t < k);
-        if (by_p) {
-            if (k)
-                all = total;
-            else
-                (void)block_before<kWaves>(z, all, sh.scratch);
-            const double limit = double(top_p) * double(all);
-            if (!k && double(total) < limit) return false;
-            keep = keep && begins(before, limit);
-        }
+        bool keep = ranked && (!(top_p < 1.f) || begins(before, double(top_p) * double(total)));
         const u64 order_t = t < n ? sh.r_order[t] : 0;
         const float w = t < n ? wt.weight(key_logit(order_key(order_t))) : 0.f;
         keep = keep && w >= min_w;
@@ -353,8 +375,8 @@ struct Sampler {
         (void)block_before<kWaves>(keep ? share : 0, W, sh.scratch);
         if (keep) atomicMax(&sh.best, t);
         __syncthreads();
-        const int kept = sh.best + 1;
-        const double target = double(fmaxf(u, 0.f)) * double(W);
+        const int kept = uniform(sh.best) + 1;
+        const double target = double(fmaxf(p.u[blockIdx.x], 0.f)) * double(W);
         if (t < kept) {
             u64 upto = 0;
             const unsigned me = unsigned(order_t);
@@ -362,8 +384,8 @@ struct Sampler {
             // the first that exceeds the target; u of 1 and more ends at the last with any weight
             const bool hit = share && !(double(upto - share) > target) && (double(upto) > target || upto == W);
             if (hit) {
-                *token = order_index(order_t);
-                if (logprob) *logprob = float(log(ldexp(double(w), frac) / double(W)));
+                p.token[blockIdx.x] = order_index(order_t);
+                if (p.logprob) p.logprob[blockIdx.x] = float(log(ldexp(double(w), p.frac) / double(W)));
             }
         }
         return true;
@@ -384,7 +406,7 @@ struct Sampler {
         };
         each([&](int f, const float x[N]) { eq += equals(f, x); });
         for (int o = 32; o; o >>= 1) eq += __shfl_xor(eq, o);
-        const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+        const int lane = threadIdx.x & 63, w = uniform(int(threadIdx.x >> 6));
         __syncthreads();
         if (lane == 0) sh.scratch[w] = eq;
         __syncthreads();
@@ -392,54 +414,62 @@ struct Sampler {
         for (int i = 0; i < w; ++i) before += sh.scratch[i];
         if (before < need && need <= before + eq) {
             for (int i = v0; i < v1; i += 64) {
-                float x[N];
+                typename Row<E>::V v{};
                 int n = 0;
                 if (i + lane < v1) {
-                    row.load(i + lane, x);
-                    n = equals(row.first(i + lane), x);
+                    v = row.raw(i + lane);
+                    row.fours(i + lane, v, [&](int f, const float x[N]) { n += equals(f, x); });
                 }
                 const u64 incl = wave_incl(u64(n)), at = before + incl - n;
                 if (at < need && need <= at + n) {
                     u64 c = at;
+                    row.fours(i + lane, v, [&](int f, const float x[N]) {
 #pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (logit_key(x[e]) == key && in(within, row.first(i + lane) + e, key) && ++c == need) sh.index = row.first(i + lane) + e;
+                        for (int e = 0; e < N; ++e)
+                            if (logit_key(x[e]) == key && in(within, f + e, key) && ++c == need) sh.index = f + e;
+                    });
                 }
                 before += __shfl(incl, 63);
                 if (before >= need) break;
             }
         }
         __syncthreads();
-        return Cut{key, sh.index};
+        return Cut{key, uniform(sh.index)};
     }
 };
 
-// One workgroup a row: the largest logit; where a rule asks for it counts and
-// weights in bins by distance from it, and the cuts; the kept weights of each
-// wave's stretch of the row; the stretch that the random number falls in.  The
-// row is read four to six times, after the first from the caches: no more of
-// 512 rows of 200 KB fits the registers, and passes unrolled over registers
-// would not fit the instruction cache.
+// One workgroup a row: the largest logit; where a rule asks for it counts or
+// weights in bins by distance from it, and the cut, whose search sums the kept
+// weights of each wave's stretch of the row; else a pass that sums them; the
+// stretch that the random number falls in, divided among the waves once more.
+// The row is read two to five times, after the first from the caches: no more
+// of 512 rows of 200 KB fits the registers.  What bounds it are the
+// instructions of two exponentials a logit, and for a single row the steps
+// between the passes.  What all lanes have alike is kept in scalar registers:
+// with vector registers spilled to memory and twice the code 512 rows of
+// 100003 logits took 230 us, one row of 32768 54 us; now 137 and 37 us (rules
+// mixed, and top-p).
 template <class E, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 4) void k_sample(const SampleP p)
 {
-    constexpr int N = Row<E>::N;
     using S = Sampler<E, kWaves>;
+    constexpr int N = S::N, kVector = Row<E>::N;
     __shared__ typename S::Shared sh;
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
     const Row<E> row(p.logits + b * p.row_bytes, p.vocab);
     const int seg = ((row.nvec + kWaves * 64 - 1) / (kWaves * 64)) * 64;
     const int v0 = min(w * seg, row.nvec), v1 = min(v0 + seg, row.nvec);
     Weigher wt;
     S s{row, wt, sh, v0, v1, Cut{0, 0x7fffffff}};
 
-    // the largest logit and its lowest index
+    // the largest logit, and the first four elements that it is among
     float best = -__builtin_inff();
     int at = 0x7fffffff;
     s.each([&](int f, const float x[N]) {
+        float m = x[0];
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (x[e] > best) best = x[e], at = f + e;
+        for (int e = 1; e < N; ++e) m = fmaxf(m, x[e]);
+        if (m > best) best = m, at = f;
     });
     const float most = best;  // of this thread
     for (int o = 32; o; o >>= 1) {
@@ -447,46 +477,67 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_sample(const SampleP p)
         const int a = __shfl_xor(at, o);
         if (k > best || (k == best && a < at)) best = k, at = a;
     }
-    if (lane == 0) sh.c_share[w] = u64(__float_as_uint(best)) << 32 | unsigned(at);
+    if (lane == 0) sh.r_share[w] = u64(__float_as_uint(best)) << 32 | unsigned(at);
     __syncthreads();
     for (int i = 0; i < kWaves; ++i) {
-        const float k = __uint_as_float(unsigned(sh.c_share[i] >> 32));
-        const int a = int(unsigned(sh.c_share[i]));
+        const float k = __uint_as_float(unsigned(sh.r_share[i] >> 32));
+        const int a = int(unsigned(sh.r_share[i]));
         if (k > best || (k == best && a < at)) best = k, at = a;
     }
+    best = uniform_f(best);
+    at = uniform(at);
     __syncthreads();
     const float t = p.temperature[b];
     const bool dead = best == -__builtin_inff();
     if (dead || !(t > 0.f)) {
         if (tid == 0) {
-            p.token[b] = dead ? -1 : at;
+            int token = -1;
+            if (!dead) {
+                const int i = (at + row.skip) / kVector;
+                row.fours(i, row.raw(i), [&](int f, const float x[N]) {
+#pragma unroll
+                    for (int e = N - 1; e >= 0; --e)
+                        if (f == at && x[e] == best) token = at + e;
+                });
+            }
+            p.token[b] = token;
             if (p.logprob) p.logprob[b] = dead ? -__builtin_inff() : 0.f;
         }
         return;
     }
-    wt.top = fminf(best, __FLT_MAX__);
-    wt.inv_t = fminf(fmaxf(1.f / t, __FLT_MIN__), __FLT_MAX__);
-    wt.magic = ldexp(1.5, 52 - p.frac);
-    wt.magic_bits = u64(__double_as_longlong(wt.magic));
-    const float min_w = fminf(fmaxf(p.min_p[b], 0.f), 1.f);  // the first rank always stays
+    wt.top = uniform_f(fminf(best, __FLT_MAX__));
+    wt.inv_t = uniform_f(fminf(fmaxf(1.f / t, __FLT_MIN__), __FLT_MAX__));
+    wt.magic_bits = u64(1075 - p.frac) << 52 | 1ull << 51;  // 1.5 * 2^(52 - frac)
+    wt.magic = __longlong_as_double((long long)(wt.magic_bits));
+    const float min_w = uniform_f(fminf(fmaxf(p.min_p[b], 0.f), 1.f));  // the first rank always stays
 
     // top-k by ranks, then top-p by the weights of what is left
     const int k_top = p.top_k[b];
     const float top_p = p.top_p[b];
     const bool by_k = k_top > 0 && k_top < p.vocab;
-    if ((by_k ? k_top <= kFew : top_p < 1.f) &&
-        s.draw_few(most, by_k ? k_top : 0, top_p, min_w, p.u[b], p.frac, p.token + b, p.logprob ? p.logprob + b : nullptr))
+    if (by_k && k_top <= kFew && s.draw_few(most, k_top, top_p, min_w, p))
         return;
-    bool cuts = false;
+    const bool by_p = top_p < 1.f, cuts = by_k || by_p;
+    u64 total = 0;  // of the kept weights of this thread's vectors
+    bool summed = false;
 #pragma unroll 1
-    for (int rule = 0; rule < 2; ++rule) {
-        if (!(rule ? top_p < 1.f : by_k)) continue;
+    for (int rule = by_k ? 0 : 1; rule < (by_p ? 2 : 1); ++rule) {
         s.clear();
+        u64 tail = 0;  // the last bin, which most of a row may lie in
         s.each([&](int f, const float x[N]) {
 #pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (!cuts || s.in(s.within, f + e, logit_key(x[e]))) atomicAdd(&sh.sum[int(s.bins_down(x[e]))], s.share(rule, x[e]));
+            for (int e = 0; e < N; ++e) {
+                if (rule && by_k && !s.in(s.within, f + e, logit_key(x[e]))) continue;
+                const int bin = int(s.bins_down(x[e]));
+                const u64 v = s.share(rule, x[e]);
+                if (bin == kBins - 1)
+                    tail += v;
+                else
+                    atomicAdd(&sh.sum[bin], v);
+            }
         });
+        for (int o = 32; o; o >>= 1) tail += __shfl_xor(tail, o);
+        if (lane == 0) atomicAdd(&sh.sum[kBins - 1], tail);
         __syncthreads();
         double limit = double(k_top);
         if (rule) {
@@ -496,69 +547,86 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_sample(const SampleP p)
             (void)block_before<kWaves>(mine, z, sh.scratch);
             limit = double(top_p) * double(z);
         }
-        s.within = s.find(rule, limit);
-        cuts = true;
+        s.within = s.find(rule, limit, min_w, total, summed);
     }
 
-    // a vector's kept weights, whole numbers, and their sum
-    const auto kept = [&](int f, const float x[N], u64 out[N], float ws[N]) {
-        u64 sum = 0;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            ws[e] = wt.weight(x[e]);
-            if (!(ws[e] >= min_w) || (cuts && !s.in(s.within, f + e, logit_key(x[e])))) ws[e] = 0.f;
-            out[e] = wt.fixed(ws[e]);
-            sum += out[e];
-        }
-        return sum;
+    // a kept weight; others are 0
+    const auto kept = [&](int index, float x) {
+        const float v = wt.weight(x);
+        return v >= min_w && (!cuts || s.in(s.within, index, logit_key(x))) ? v : 0.f;
     };
     // the least logit that may be kept
     // (of min_p with more than the rounding of a weight to spare)
     float least = cuts ? key_logit(s.within.key) : -__builtin_inff();
     if (min_w > 0.f) least = fmaxf(least, wt.top + (__logf(min_w) - 0.01f) * t * 1.0001f - 1e-30f);
-    const auto none = [&](const float x[N]) {
-        float m = x[0];
+    const auto sum_kept = [&](int from, int to) {
+        u64 sum = 0;
+        s.each(from, to, [&](int f, const float x[N]) {
+            if (fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) < least) return;
 #pragma unroll
-        for (int e = 1; e < N; ++e) m = fmaxf(m, x[e]);
-        return m < least;
+            for (int e = 0; e < N; ++e) sum += wt.fixed(kept(f + e, x[e]));
+        });
+        return sum;
     };
-    u64 total = 0;
-    if (cuts || min_w > 0.f) {
-        s.each([&](int f, const float x[N]) {
-            if (none(x)) return;
-            u64 out[N];
-            float ws[N];
-            total += kept(f, x, out, ws);
-        });
-    } else {
-        s.each([&](int, const float x[N]) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) total += wt.biased(wt.weight(x[e]));
-            total -= u64(N) * wt.magic_bits;
-        });
-    }
-    for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
-    __syncthreads();
-    if (lane == 0) sh.scratch[w] = total;
-    __syncthreads();
+    // The waves' sums, first of their own stretches of the row (known already where the last cut's search summed them),
+    // then of a part each of the stretch that the target falls in; the wave whose part it falls in finds the token.
     u64 W = 0, lower = 0;
-    for (int i = 0; i < kWaves; ++i) {
-        if (i < w) lower += sh.scratch[i];
-        W += sh.scratch[i];
+    double target = 0.0;
+    int from = v0, to = v1;
+#pragma unroll 1
+    for (int level = 0; level < 2; ++level) {
+        if (level || !summed) total = sum_kept(from, to);
+        for (int o = 32; o; o >>= 1) total += __shfl_xor(total, o);
+        __syncthreads();
+        if (lane == 0) sh.scratch[w] = total;
+        __syncthreads();
+        if (!level) {
+            if (summed) {
+                // the listed tokens that are kept, to the waves that have them
+                if (tid < sh.n) {
+                    const u64 o = sh.r_order[tid];
+                    const int index = S::order_index(o);
+                    const float v = kept(index, key_logit(S::order_key(o)));
+                    if (v > 0.f) atomicAdd(&sh.scratch[((index + row.skip) / kVector) / seg], wt.fixed(v));
+                }
+                __syncthreads();
+            }
+#pragma unroll 4
+            for (int i = 0; i < kWaves; ++i) W += sh.scratch[i];
+            W = uniform_u(W);
+            target = double(fmaxf(p.u[b], 0.f)) * double(W);
+        }
+        // which of the sums the target falls in, and what comes before it; u of 1 and more ends at the last with any weight
+        u64 at_sum = lower;
+        int which = 0;
+#pragma unroll 4
+        for (int i = 0; i < kWaves; ++i) {
+            const u64 v = sh.scratch[i];
+            if (v && !(double(at_sum) > target)) which = i, lower = at_sum;
+            at_sum += v;
+        }
+        which = uniform(which);
+        lower = uniform_u(lower);
+        if (level) {
+            if (which != w) return;
+        } else {
+            const int a0 = min(which * seg, row.nvec), a1 = min(a0 + seg, row.nvec);
+            const int part = ((a1 - a0 + kWaves * 64 - 1) / (kWaves * 64)) * 64;
+            from = min(a0 + w * part, a1);
+            to = min(from + part, a1);
+        }
     }
-    const double target = double(fmaxf(p.u[b], 0.f)) * double(W);
-    // the stretch that the target falls in finds the token; u of 1 and more ends at the last kept one
-    const bool here = total && !(double(lower) > target) && (double(lower + total) > target || lower + total == W);
-    if (!here) return;
     u64 run = lower;
-    for (int i = v0; i < v1; i += 64) {
+    for (int i = from; i < to; i += 64) {
         const int v = i + lane;
-        u64 out[N], mine = 0;
-        float ws[N];
-        if (v < v1) {
-            float x[N];
-            row.load(v, x);
-            if (!none(x)) mine = kept(row.first(v), x, out, ws);
+        u64 mine = 0;
+        typename Row<E>::V vec{};
+        if (v < to) {
+            vec = row.raw(v);
+            row.fours(v, vec, [&](int f, const float x[N]) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) mine += wt.fixed(kept(f + e, x[e]));
+            });
         }
         if (!__any(mine != 0)) continue;
         const u64 incl = wave_incl(mine), sum = __shfl(incl, 63), m = run + incl - mine;
@@ -570,13 +638,17 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_sample(const SampleP p)
                 u64 c = m;
                 int token = -1;
                 float weight = 0.f;
+                row.fours(v, vec, [&](int f, const float x[N]) {
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    if (!out[e] || (token >= 0 && double(c) > target)) continue;
-                    c += out[e];
-                    token = row.first(v) + e;
-                    weight = ws[e];
-                }
+                    for (int e = 0; e < N; ++e) {
+                        const float k = kept(f + e, x[e]);
+                        const u64 n = wt.fixed(k);
+                        if (!n || (token >= 0 && double(c) > target)) continue;
+                        c += n;
+                        token = f + e;
+                        weight = k;
+                    }
+                });
                 p.token[b] = token;
                 if (p.logprob) p.logprob[b] = float(log(ldexp(double(weight), p.frac) / double(W)));
             }
@@ -589,8 +661,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_sample(const SampleP p)
 template <class E>
 static void launch_sample(const SampleP& p, uint32_t rows, hipStream_t stream)
 {
-// With a row or less a compute unit, all its waves take one; else half of them, so that two rows' passes and steps between
-    // them overlap.
+    // With a row or less a compute unit, 16 waves take one; else 8, so that two rows' passes and steps between them overlap
+    // (512 rows: 137 us with 8 waves, 163 us with 16).
     if (rows <= 256)
         hipLaunchKernelGGL((k_sample<E, 16>), dim3(rows), dim3(1024), 0, stream, p);
     else
