@@ -20,14 +20,16 @@ constexpr int kWeighRound = 128;  // keys of one round of a workgroup: 4 waves x
 
 // A key's weight is one job's alone, so nothing is joined.  A wave holds 32
 // keys, straight from memory in the matrix instruction's layout, and passes
-// over the query rows, 32 at a time, which lie in LDS (all of a request's, or
-// ROWS of them in turn where there are more).  A lane's scores S^T = K Q^T are
+// over the query rows, 32 at a time, which lie in LDS.  Where a request has
+// more than the ROWS that fit, the job passes over its keys again for the next
+// ROWS, whose weights add to what the first pass stored (staged anew for every
+// 128 keys instead, windows of 64 tokens and 4 heads took 67 us, now 42 us).  A lane's scores S^T = K Q^T are
 // 16 keys of one query: weights add up in the lane, and over the 32 lanes at
 // the end, where each step of the exchange halves what a lane still holds.
 template <class T, int D>
 __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void k_weigh(const WeighP p)
 {
-    constexpr int KS = D / 16, CH = D / 8, ROWS = D == 256 ? 64 : 128;
+    constexpr int KS = D / 16, CH = D / 8, ROWS = 16384 / D / 32 * 32;
     __shared__ __attribute__((aligned(16))) char qs[ROWS * D * 2];
     __shared__ float refs[ROWS];
     __shared__ int64_t scratch[8];
@@ -70,20 +72,19 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void k_weigh(const WeighP p)
             for (int s = 0; s < KS; ++s) kn[s] = *reinterpret_cast<const s16x8*>(kp + (2 * s + h) * 16);
             load_id(k0 + kWeighRound);
         };
-        load_id(j.k0 + 32 * w);
-        load_keys(j.k0 + 32 * w);
-        if (rows <= ROWS) stage(0);
-        for (int kr = j.k0; kr < j.k1; kr += kWeighRound) {
-            const int k0 = kr + 32 * w, id = id_next;
-            s16x8 kf[KS];
-#pragma unroll
-            for (int s = 0; s < KS; ++s) kf[s] = kn[s];
-            if (kr + kWeighRound < j.k1) load_keys(k0 + kWeighRound);
-            float acc[16] = {};
-            const bool fresh = k0 + 32 > base;
 #pragma unroll 1
-            for (int row0 = 0; row0 < rows; row0 += ROWS) {
-                if (rows > ROWS) stage(row0);
+        for (int row0 = 0; row0 < rows; row0 += ROWS) {
+            load_id(j.k0 + 32 * w);
+            load_keys(j.k0 + 32 * w);
+            stage(row0);
+            for (int kr = j.k0; kr < j.k1; kr += kWeighRound) {
+                const int k0 = kr + 32 * w, id = id_next;
+                s16x8 kf[KS];
+#pragma unroll
+                for (int s = 0; s < KS; ++s) kf[s] = kn[s];
+                if (kr + kWeighRound < j.k1) load_keys(k0 + kWeighRound);
+                float acc[16] = {};
+                const bool fresh = k0 + 32 > base;
 #pragma unroll 1
                 for (int r = 0; r < ROWS && row0 + r < rows; r += 32) {
                     const float ref = refs[r + lq];
@@ -109,28 +110,29 @@ __global__ __launch_bounds__(256, D == 256 ? 2 : 3) void k_weigh(const WeighP p)
                         for (int i = 0; i < 16; ++i) acc[i] += exp2_fast(__builtin_fmaf(sc[i], p.scale2, -ref));
                     }
                 }
-            }
-            // bit 4 of the lane's number keeps the upper or lower eight sums, bit 3 of these the upper or lower four, ...
-            // (sums 8 and 4 stand for keys 16 and 8, sums 2 and 1 for keys 2 and 1)
-            int key = k0 + 4 * h;
-            const auto halve = [&](auto bit, auto n, auto keys) {
-                const bool up = lane & bit;
+                // bit 4 of the lane's number keeps the upper or lower eight sums, bit 3 of these the upper or lower four, ...
+                // (sums 8 and 4 stand for keys 16 and 8, sums 2 and 1 for keys 2 and 1)
+                int key = k0 + 4 * h;
+                const auto halve = [&](auto bit, auto n, auto keys) {
+                    const bool up = lane & bit;
 #pragma unroll
-                for (int i = 0; i < n; ++i) {
-                    const float keep = up ? acc[n + i] : acc[i], give = up ? acc[i] : acc[n + i];
-                    acc[i] = keep + __shfl_xor(give, bit);
+                    for (int i = 0; i < n; ++i) {
+                        const float keep = up ? acc[n + i] : acc[i], give = up ? acc[i] : acc[n + i];
+                        acc[i] = keep + __shfl_xor(give, bit);
+                    }
+                    key += up ? keys : 0;
+                };
+                halve(Int<16>(), Int<8>(), Int<16>());
+                halve(Int<8>(), Int<4>(), Int<8>());
+                halve(Int<4>(), Int<2>(), Int<2>());
+                halve(Int<2>(), Int<1>(), Int<1>());
+                const float mine = acc[0] + __shfl_xor(acc[0], 1);
+                const int block = __shfl(id, (key - k0) & 31);  // the lane that loaded the key knows its block
+                if (!(lane & 1) && block >= 0) {
+                    float* at = p.score + ((size_t(block) * p.pool.kv_heads + j.hk) << p.pool.lb) + (key & omask);
+                    const float kept = row0 ? 1.f : p.decay == 0.f || key >= base ? 0.f : p.decay;
+                    *at = kept == 0.f ? mine : kept * *at + mine;
                 }
-                key += up ? keys : 0;
-            };
-            halve(Int<16>(), Int<8>(), Int<16>());
-            halve(Int<8>(), Int<4>(), Int<8>());
-            halve(Int<4>(), Int<2>(), Int<2>());
-            halve(Int<2>(), Int<1>(), Int<1>());
-            const float mine = acc[0] + __shfl_xor(acc[0], 1);
-            const int block = __shfl(id, (key - k0) & 31);  // the lane that loaded the key knows its block
-            if (!(lane & 1) && block >= 0) {
-                float* at = p.score + ((size_t(block) * p.pool.kv_heads + j.hk) << p.pool.lb) + (key & omask);
-                *at = p.decay == 0.f || key >= base ? mine : p.decay * *at + mine;
             }
         }
     }
