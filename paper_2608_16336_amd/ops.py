@@ -108,11 +108,11 @@ def _packer(cls):
                 yield from codes(t)
             else:
                 yield {_vp: "P", _u32: "I", _i64: "q", _f32: "f", _size: "N"}[t]
-    s = struct.Struct("@" + "".join(codes(cls)))
-    if ctypes.sizeof(cls) - s.size not in range(8):
+    form = "@" + "".join(codes(cls))
+    tail = ctypes.sizeof(cls) - struct.calcsize(form)
+    if tail not in range(8):
         raise AssertionError(cls)
-    tail = bytes(ctypes.sizeof(cls) - s.size)
-    return (lambda *v: s.pack(*v) + tail) if tail else s.pack
+    return struct.Struct(form + "x" * tail).pack
 
 
 _rope_pack, _attend_pack, _weigh_pack, _evict_pack, _sample_pack = (
@@ -120,31 +120,40 @@ _rope_pack, _attend_pack, _weigh_pack, _evict_pack, _sample_pack = (
 _INT32, _INT64, _FLOAT32, _FLOAT64 = torch.int32, torch.int64, torch.float32, torch.float64
 
 
+# A call's GPU goes by its number: comparing device objects takes several
+# times as long, and with a dozen tensors a call a decode step waits for it.
+
+def _gpu(t):
+    device = t.get_device()
+    if device < 0:
+        raise ValueError("tensors must be on a GPU")
+    return device
+
+
 def _device(t, what, device, dtype, shape):
     """The address of a contiguous tensor of one type and shape on the call's GPU."""
-    if t.dtype is not dtype or t.shape != shape or t.device != device or not t.is_contiguous():
-        raise ValueError("%s: contiguous %s %s on %s, got %s %s on %s" % (what, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise ValueError("%s: contiguous %s %s on cuda:%d, got %s %s on %s" % (
+            what, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.device))
     return t.data_ptr()
 
 
 def _rows(t, what, device, dtype):
     """[tokens][heads][dim] with the last dimension contiguous: (token, head) strides."""
     s = t.stride()
-    if len(s) != 3 or t.dtype is not dtype or t.device != device or (s[2] != 1 and t.shape[2] != 1):
-        raise ValueError("%s: [tokens][heads][dim] of %s on %s, last dimension contiguous" % (what, dtype, device))
+    if len(s) != 3 or t.dtype is not dtype or t.get_device() != device or (s[2] != 1 and t.shape[2] != 1):
+        raise ValueError("%s: [tokens][heads][dim] of %s on cuda:%d, last dimension contiguous" % (what, dtype, device))
     return s[0], s[1]
 
 
 def _call(name, packed, device):
-    if device.type != "cuda":
-        raise ValueError("tensors must be on a GPU")
-    fn, i = getattr(_lib or _library(), name), device.index
+    fn = getattr(_lib or _library(), name)
     # the launch goes to the tensors' GPU, whatever the current one is
-    if i == torch._C._cuda_getDevice():
-        rc = fn(packed, torch._C._cuda_getCurrentRawStream(i))
+    if device == torch._C._cuda_getDevice():
+        rc = fn(packed, torch._C._cuda_getCurrentRawStream(device))
     else:
         with torch.cuda.device(device):
-            rc = fn(packed, torch._C._cuda_getCurrentRawStream(i))
+            rc = fn(packed, torch._C._cuda_getCurrentRawStream(device))
     if rc:
         raise MtsError(name, rc)
 
@@ -154,12 +163,12 @@ def _pool(k, v, device, dtype, heads=None, dim=None):
     shape, s = k.shape, k.stride()
     if len(shape) != 4 or s[3] != 1 or k.dtype not in TYPES:
         raise ValueError("a pool is [blocks][kv_heads][block_tokens][head_dim] of bfloat16 or float16, last dimension contiguous")
-    if k.device != device or k.dtype is not dtype or (dim is not None and shape[3] != dim) or (heads is not None and shape[1] != heads):
+    if k.get_device() != device or k.dtype is not dtype or (dim is not None and shape[3] != dim) or (heads is not None and shape[1] != heads):
         raise ValueError("the pool differs from the call's other tensors in heads, head dimension, type or device")
     at, z = 0, (0, 0, 0)
     if v is not None:
         z = v.stride()
-        if v.shape != shape or v.dtype is not dtype or v.device != device or z[3] != 1:
+        if v.shape != shape or v.dtype is not dtype or v.get_device() != device or z[3] != 1:
             raise ValueError("v_cache must match k_cache")
         at = v.data_ptr()
     return k.data_ptr(), at, s[0], s[1], s[2], z[0], z[1], z[2], shape[0], shape[2], shape[1], shape[3], TYPES[dtype], 0
@@ -201,41 +210,46 @@ def _rope(q, k, v, positions, slots, freqs, pool, pos, layout, mscale, inverse, 
     any_ = q if q is not None else k
     if any_ is None:
         raise ValueError("q or k")
-    device, dtype = any_.device, any_.dtype
+    device, dtype = _gpu(any_), any_.dtype
     if dtype not in TYPES or any_.dim() != 3:
         raise ValueError("[tokens][heads][dim] of bfloat16, float16 or float32")
     n, _, D = any_.shape
-    at, strides = [], []
-    for x, what in ((q, "q"), (k, "k"), (v, "v")):
-        if x is None:
-            at.append(0)
-            strides += (0, 0)
-            continue
-        strides += _rows(x, what, device, dtype)
-        if x.shape[0] != n or x.shape[2] != D:
+    qp = kp = vp = qo = ko = Hq = Hk = 0
+    qs = ks = vs = qos = kos = (0, 0)
+    if q is not None:
+        qs, qp = _rows(q, "q", device, dtype), q.data_ptr()
+        shape = q.shape
+        Hq = shape[1]
+        if q_out is None:
+            q_out = torch.empty(shape, dtype=dtype, device=device)
+            qos = Hq * D, D
+        else:
+            qos = _rows(q_out, "q_out", device, dtype)
+            if q_out.shape != shape:
+                raise ValueError("q_out: the shape of its input")
+        qo = q_out.data_ptr()
+    if k is not None:
+        ks, kp = _rows(k, "k", device, dtype), k.data_ptr()
+        shape = k.shape
+        Hk = shape[1]
+        if shape[0] != n or shape[2] != D:
             raise ValueError("q, k and v differ in tokens or head dimension")
-        at.append(x.data_ptr())
-    if q is not None and q_out is None:
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    if k is not None and k_out is None and slots is None:
-        k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-    for x, y, what in ((q, q_out, "q_out"), (k, k_out, "k_out")):
-        if x is None or y is None:
-            at.append(0)
-            strides += (0, 0)
-            continue
-        strides += _rows(y, what, device, dtype)
-        if y.shape != x.shape:
-            raise ValueError("%s: the shape of its input" % what)
-        at.append(y.data_ptr())
+        if k_out is None and slots is None:
+            k_out = torch.empty(shape, dtype=dtype, device=device)
+        if k_out is not None:
+            kos, ko = _rows(k_out, "k_out", device, dtype), k_out.data_ptr()
+            if k_out.shape != shape:
+                raise ValueError("k_out: the shape of its input")
+    if v is not None:  # rope_append() has compared its shape with k's
+        vs, vp = _rows(v, "v", device, dtype), v.data_ptr()
     if freqs.dim() != 1:
         raise ValueError("freqs: [rot / 2]")
     if pool is None:
-        pool = _NO_POOL + (0 if k is None else k.shape[1], D, TYPES[dtype], 0)
+        pool = _NO_POOL + (Hk, D, TYPES[dtype], 0)
     _call("mts_rope", _rope_pack(
-        *at, *strides, _device(positions, "positions", device, _INT32, (n,)), _device(freqs, "freqs", device, _FLOAT64, freqs.shape),
-        0 if slots is None else _device(slots, "slots", device, _INT64, (n,)), pos, *pool, n, 0 if q is None else q.shape[1],
-        2 * freqs.shape[0], LAYOUTS[layout], 1 if inverse else 0, mscale), device)
+        qp, kp, vp, qo, ko, *qs, *ks, *vs, *qos, *kos, _device(positions, "positions", device, _INT32, (n,)),
+        _device(freqs, "freqs", device, _FLOAT64, freqs.shape), 0 if slots is None else _device(slots, "slots", device, _INT64, (n,)), pos,
+        *pool, n, Hq, 2 * freqs.shape[0], LAYOUTS[layout], 1 if inverse else 0, mscale), device)
     return q_out, k_out
 
 
@@ -254,7 +268,7 @@ def rope_append(q, k, v, positions, slots, freqs, k_cache, v_cache, pos=None, *,
         raise ValueError("k and slots")
     if v is not None and (v.shape != k.shape or v_cache is None):
         raise ValueError("v: the shape of k, and v_cache")
-    device = k.device
+    device = _gpu(k)
     pool = _pool(k_cache, v_cache, device, k.dtype, k.shape[1], k.shape[2])
     at = 0 if pos is None else _device(pos, "pos", device, _INT32, k_cache.shape[:3])
     return _rope(q, k, v, positions, slots, freqs, pool, at, layout, mscale, False, q_out, None)[0]
@@ -278,7 +292,7 @@ def attend(q, k_cache, v_cache, table, lens, q_start, max_q, *, scale=None, tree
     attend those before them and themselves.  scale: dim ** -0.5 by default.
     workspace: a uint8 tensor of at least attend_workspace() bytes that no other
     stream uses meanwhile; by default one is taken for the call."""
-    device, dtype = q.device, q.dtype
+    device, dtype = _gpu(q), q.dtype
     strides = _rows(q, "q", device, dtype)
     N, Hq, D = q.shape
     pool = _pool(k_cache, v_cache, device, dtype, None, D)
@@ -294,13 +308,15 @@ def attend(q, k_cache, v_cache, table, lens, q_start, max_q, *, scale=None, tree
             raise ValueError("out: the shape of q")
     if lse is None:
         lse = torch.empty((N, Hq), dtype=_FLOAT32, device=device)
+        sums = lse.data_ptr()
+    else:
+        sums = _device(lse, "lse", device, _FLOAT32, (N, Hq))
     if workspace is None:
         workspace = torch.empty(attend_workspace(lens.shape[0], N, max_q, Hq, k_cache.shape[1], D), dtype=torch.uint8, device=device)
-    elif workspace.device != device or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
-        raise ValueError("workspace: contiguous uint8 on %s" % device)
+    elif workspace.get_device() != device or workspace.dtype is not torch.uint8 or not workspace.is_contiguous():
+        raise ValueError("workspace: contiguous uint8 on cuda:%d" % device)
     _call("mts_attend", _attend_pack(
-        *pool, *batch, q.data_ptr(), out.data_ptr(), _device(lse, "lse", device, _FLOAT32, (N, Hq)), *strides, *outs, Hq,
-        D ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel()), device)
+        *pool, *batch, q.data_ptr(), out.data_ptr(), sums, *strides, *outs, Hq, D ** -0.5 if scale is None else scale, workspace.data_ptr(), workspace.numel()), device)
     return out, lse
 
 
@@ -311,7 +327,7 @@ def weigh(q, lse, k_cache, table, lens, q_start, max_q, score, *, scale=None, de
     """Adds to score [blocks][kv_heads][block_tokens] float32 (times decay) the
     softmax weights that every slot gets from the new tokens' queries, lse being
     attend()'s; returns score.  The new tokens' own slots start from zero."""
-    device, dtype = q.device, q.dtype
+    device, dtype = _gpu(q), q.dtype
     strides = _rows(q, "q", device, dtype)
     N, Hq, D = q.shape
     _call("mts_weigh", _weigh_pack(
@@ -335,7 +351,7 @@ def evict(k_cache, v_cache, score, pos, table, lens, next_pos, budget, *, recent
     first `sink` and last `recent` positions, then the largest scores.  Kept
     rows above the budget move into the holes below it, in the pool, score_out
     and pos_out (by default score and pos themselves); returns the new lens."""
-    device = k_cache.device
+    device = _gpu(k_cache)
     pool = _pool(k_cache, v_cache, device, k_cache.dtype)
     if v_cache is None:
         raise ValueError("v_cache")
@@ -366,7 +382,7 @@ def sample(logits, u, temperature, top_k, top_p, min_p, *, token=None, logprob=N
     -inf gives token -1."""
     if logits.dim() != 2 or logits.dtype not in TYPES or (logits.stride(1) != 1 and logits.shape[1] != 1):
         raise ValueError("logits: [rows][vocab] of bfloat16, float16 or float32, rows contiguous")
-    device, (rows, vocab) = logits.device, logits.shape
+    device, (rows, vocab) = _gpu(logits), logits.shape
     if token is None:
         token = torch.empty(rows, dtype=_INT32, device=device)
     if logprob is None:
