@@ -236,17 +236,19 @@ __device__ __forceinline__ int64_t uniform(int64_t x)
 // The jobs of a ragged batch.  Lengths live on the device, so every workgroup
 // (NW waves) of a launch finds out for itself what there is to do: it sums the
 // requests' rounds and takes as many rounds a job as leave about `target`
-// jobs.  Jobs are numbered head by head, in it request by request, longest
-// first (as far as there is one a thread; more are passed over in turns), in
-// it split by split and group by group.
+// jobs, the rounds of a request divided evenly.  Jobs are numbered head by
+// head, in it request by request, longest jobs first (as far as there is one a
+// thread; more are passed over in turns), in it split by split and group by
+// group.
 //
 // A workgroup takes several jobs: the launch has as many workgroups as the
 // chip holds at once, because one a job, given out by the hardware in turns,
 // left compute units idle (a fifth of the time of equal chunks of prompts).
 // Each of the 8 dies (workgroups go to them in turn) has an eighth of the
-// numbers, so that jobs of a head, which share keys, share a cache; in it the
-// workgroups count forth and back, so that who began with a long job ends with
-// a short one.
+// numbers, so that jobs of a head, which share keys, share a cache.  A die's
+// first 32 workgroups go to one compute unit each, the next 32 beside them, and
+// so on; they count forth and back, and so do the turns: who has a long job
+// shares its unit with a short one, and takes a short one next.
 template <int NW>
 struct Jobs {
     static constexpr int NT = 64 * NW;
@@ -266,7 +268,10 @@ struct Jobs {
     {
         return b.n <= NT ? share_with(s, r, said[r], said[NT + r], said[2 * NT + r]) : share_of(p, b, s, r);
     }
-    __device__ __forceinline__ int64_t count(const Share& x) const { return int64_t((x.rounds + per - 1) / per) * x.groups; }
+    // splits of a request's rounds, and the rounds of one (the last one's may be fewer)
+    __device__ __forceinline__ int splits(int rounds) const { return (rounds + per - 1) / per; }
+    __device__ __forceinline__ int each(int rounds) const { return (rounds + splits(rounds) - 1) / splits(rounds); }
+    __device__ __forceinline__ int64_t count(const Share& x) const { return int64_t(splits(x.rounds)) * x.groups; }
 
     __device__ __forceinline__ Jobs(const Pool& p_, const Batch& b_, const SplitRule& s_, int64_t* scratch_) : p(p_), b(b_), s(s_), scratch(scratch_)
     {
@@ -287,14 +292,15 @@ struct Jobs {
         per = uniform(total > s.target ? int((total + s.target - 1) / s.target) : 1);
         if (b.n <= NT) {
             int* len = reinterpret_cast<int*>(before);
-            len[t] = q.rounds;
+            const int mine = q.rounds ? each(q.rounds) : 0;
+            len[t] = mine;
             said[t] = q.L;
             said[NT + t] = q.T;
             said[2 * NT + t] = q.first;
             __syncthreads();
             if (t < b.n) {
                 int rank = 0;
-                for (int i = 0; i < b.n; ++i) rank += len[i] > q.rounds || (len[i] == q.rounds && i < t);
+                for (int i = 0; i < b.n; ++i) rank += len[i] > mine || (len[i] == mine && i < t);
                 order[rank] = t;
             }
             __syncthreads();
@@ -334,8 +340,9 @@ struct Jobs {
     // The turn-th job of this workgroup; false past the last one.  Uniform, with barriers.
     __device__ __forceinline__ bool get(int turn, Job& j)
     {
-        const int64_t chunk = (jobs + 7) / 8, wide = gridDim.x >> 3, at = blockIdx.x >> 3;
-        const int64_t local = turn * wide + (turn & 1 ? wide - 1 - at : at), id = (blockIdx.x & 7) * chunk + local;
+        const int chip = 32, wide = gridDim.x >> 3, b0 = blockIdx.x >> 3, row = b0 / chip, last_row = min(chip, wide - row * chip) - 1;
+        const int64_t chunk = (jobs + 7) / 8, at = row & 1 ? row * chip + last_row - b0 % chip : b0;
+        const int64_t local = int64_t(turn) * wide + (turn & 1 ? wide - 1 - at : at), id = (blockIdx.x & 7) * chunk + local;
         if (local >= chunk || id >= jobs) return false;
         const int t = threadIdx.x, hk = int(id / head);
         const int64_t in = id % head;
@@ -363,10 +370,10 @@ struct Jobs {
         j.L = uniform(q.L);
         j.T = uniform(q.T);
         j.first = uniform(q.first);
-        j.nsplit = (rounds + per - 1) / per;
+        j.nsplit = splits(rounds);
         j.split = i / j.step;
         j.grp = i % j.step;
-        const int64_t k0 = int64_t(j.split) * per * s.unit, k1 = k0 + int64_t(per) * s.unit;
+        const int64_t k0 = int64_t(j.split) * each(rounds) * s.unit, k1 = k0 + int64_t(each(rounds)) * s.unit;
         j.k0 = int(k0);
         j.k1 = int(k1 < j.L ? k1 : j.L);
         return true;
