@@ -684,8 +684,8 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void k_attend_tiles(cons
 // Rows of 256 elements leave room for four waves only.
 //
 // Jobs to aim for: two a compute unit for the stream (a decode of 150 requests
-// takes 122, 100, 105, 111 us at 256, 512, 1024, 2048), one for the tiles (265
-// us the trees, 284 us at 512), whose parts are large.
+// takes 122, 100, 105, 111 us at 256, 512, 1024, 2048), fewer for the tiles,
+// whose parts are large (the trees 225, 220, 238 us at 256, 384, 512).
 struct Sizes {
     uint32_t rows;    // query rows of a job
     uint32_t target;  // jobs to aim for
@@ -699,7 +699,7 @@ static Sizes sizes(uint32_t n, uint32_t n_tokens, uint32_t max_q, uint32_t q_hea
     Sizes s;
     const uint64_t most = uint64_t(max_q) * G;
     s.rows = most <= 16 ? 16 : most <= 256 || head_dim == 256 ? 128 : 256;
-    s.target = s.rows == 16 ? 512 : 256;
+    s.target = s.rows == 16 ? 512 : 384;
     s.jobs = max_jobs(n, n_tokens, kv_heads, G, s.rows, s.target);
     s.part = 256;
     s.ml = s.part + align256(sizeof(Part) * s.jobs);
