@@ -189,7 +189,8 @@ int mts_evict_workspace(uint32_t n, uint32_t kv_heads, uint32_t table_width, uin
  * exceeds u times the kept sum; sums are carried in 64 bits.  logprob is the
  * logarithm of its share of the kept sum.  temperature <= 0: the first rank,
  * logprob 0.  NaN counts as -inf; a row without any larger logit gives -1 and
- * -inf.  Logits of +inf share the whole weight. */
+ * -inf.  Logits of +inf share the whole weight.  Rows are read in whole
+ * aligned pieces of 16 bytes, at their ends with what lies beside them. */
 typedef struct mts_sample_args {
     const void* logits;           /* [rows][vocab], row_stride apart */
     int64_t row_stride;
