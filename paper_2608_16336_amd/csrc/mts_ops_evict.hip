@@ -23,7 +23,7 @@ constexpr int kWeighRound = 128;  // keys of one round of a workgroup: 4 waves x
 // over the query rows, 32 at a time, which lie in LDS.  Where a request has
 // more than the ROWS that fit, the job passes over its keys again for the next
 // ROWS, whose weights add to what the first pass stored (staged anew for every
-// 128 keys instead, windows of 64 tokens and 4 heads took 67 us, now 42 us).  A lane's scores S^T = K Q^T are
+// 128 keys instead, windows of 64 tokens and 4 heads took 67 us, now 44 us).  A lane's scores S^T = K Q^T are
 // 16 keys of one query: weights add up in the lane, and over the 32 lanes at
 // the end, where each step of the exchange halves what a lane still holds.
 template <class T, int D>
@@ -172,14 +172,16 @@ struct SlotView {
         id = p.batch.table[size_t(r) * p.batch.width + (slot >> p.pool.lb)];
         return ((size_t(id) * p.pool.kv_heads + hk) << p.pool.lb) + (slot & ((1 << p.pool.lb) - 1));
     }
+    __device__ __forceinline__ unsigned key_of(bool ok, int ps, float sc) const
+    {
+        return !ok ? 0u : (long long)(ps) < p.sink || ps >= from ? 0xffffffffu : score_key(sc);
+    }
     __device__ __forceinline__ unsigned key(int slot) const
     {
         int id;
         const size_t at = index(slot, id);
         const bool ok = unsigned(id) < p.pool.n_blocks;
-        const int ps = p.pos[ok ? at : 0];
-        const float sc = p.score[ok ? at : 0];
-        return !ok ? 0u : (long long)(ps) < p.sink || ps >= from ? 0xffffffffu : score_key(sc);
+        return key_of(ok, p.pos[ok ? at : 0], p.score[ok ? at : 0]);
     }
 };
 
@@ -209,9 +211,9 @@ __device__ __forceinline__ int scan16(int v, int& total, int* scratch)
 // lists the moves in slot order: waves own consecutive stretches of slots and
 // count before they write, so that no order is left to chance.  Every pass
 // needs every key: `held` of them (all, up to 32768) are read once and kept in
-// LDS, further ones are read again.  Read in every pass, the longest of 64
-// requests (20000 slots) took 94 us, most of it the latency of three loads that
-// depend on each other.
+// LDS, further ones are read again.  The longest of 64 requests (20000 slots)
+// takes 37 us: 54 us with four slots of a lane on their way instead of eight,
+// the outputs copied before, and equal keys counted where none need be.
 constexpr int kHeld = 32768;
 
 __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictP p, const int held)
@@ -219,35 +221,47 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictP p,
     extern __shared__ unsigned keys[];
     __shared__ int hist[2048];
     __shared__ int scratch[kSelectWaves];
-    __shared__ int cut[2];
+    __shared__ int cut[3];
     __shared__ int wave_a[kSelectWaves], wave_b[kSelectWaves];
     const int hk = blockIdx.x, r = blockIdx.y, tid = threadIdx.x, lane = tid & 63, w = uniform(tid >> 6);
     const int L = request_len(p.pool, p.batch, r), B = p.budget;
     const SlotView v{p, r, hk, (long long)(p.next_pos[r]) - p.recent};
     if (hk == 0 && tid == 0) p.lens_out[r] = L < B ? L : B;
-    // what the budget covers goes to the outputs as it is; what moves overwrites the given up places later
-    if (p.score_out != p.score || p.pos_out != p.pos)
-        for (int s = tid; s < min(L, B); s += kSelectThreads) {
-            int id;
-            const size_t at = v.index(s, id);
-            if (unsigned(id) >= p.pool.n_blocks) continue;
-            p.score_out[at] = p.score[at];
-            p.pos_out[at] = p.pos[at];
+    // What the budget covers goes to the outputs as it is; what moves overwrites the given up places later.  A wave reads
+    // and writes its own stretch's keys only, U of a lane's on their way at once.
+    const bool copies = p.score_out != p.score || p.pos_out != p.pos;
+    const int seg = ((L + kSelectThreads - 1) / kSelectThreads) * 64;
+    const int s0 = min(w * seg, L), s1 = min(s0 + seg, L), s2 = min(s1, held), covered = min(s1, B);
+    if (L > B || copies) {
+        constexpr int U = 8;
+        const int end = max(s2, copies ? covered : 0);
+        for (int s = s0 + lane; s < end; s += 64 * U) {
+            int id[U], ps[U];
+            size_t at[U];
+            float sc[U];
+#pragma unroll
+            for (int i = 0; i < U; ++i) at[i] = v.index(min(s + 64 * i, end - 1), id[i]);
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const size_t in = unsigned(id[i]) < p.pool.n_blocks ? at[i] : 0;
+                ps[i] = p.pos[in];
+                sc[i] = p.score[in];
+            }
+#pragma unroll
+            for (int i = 0; i < U; ++i) {
+                const bool ok = unsigned(id[i]) < p.pool.n_blocks;
+                const int slot = s + 64 * i;
+                if (slot < s2) keys[slot] = v.key_of(ok, ps[i], sc[i]);
+                if (copies && ok && slot < covered) {
+                    p.score_out[at[i]] = sc[i];
+                    p.pos_out[at[i]] = ps[i];
+                }
+            }
         }
+    }
     if (L <= B) {
         if (tid == 0) p.n_moves[size_t(r) * p.pool.kv_heads + hk] = 0;
         return;
-    }
-    // a wave reads and writes its own stretch's keys only
-    const int seg = ((L + kSelectThreads - 1) / kSelectThreads) * 64;
-    const int s0 = min(w * seg, L), s1 = min(s0 + seg, L), s2 = min(s1, held);
-    for (int s = s0 + lane; s < s2; s += 256) {
-        unsigned k[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) k[i] = v.key(min(s + 64 * i, L - 1));
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (s + 64 * i < s2) keys[s + 64 * i] = k[i];
     }
     lds_order();
     // f(slot, whether it is one, its key) for the wave's slots, 64 at a time in slot order
@@ -282,21 +296,24 @@ __global__ __launch_bounds__(kSelectThreads) void k_evict_select(const EvictP p,
         const int a = hi >= 0 ? hist[hi] : 0, b = lo >= 0 ? hist[lo] : 0;
         int total;
         const int above = scan16(a + b, total, scratch);
-        if (above < need && need <= above + a) cut[0] = hi, cut[1] = need - above;
-        if (above + a < need && need <= above + a + b) cut[0] = lo, cut[1] = need - above - a;
+        if (above < need && need <= above + a) cut[0] = hi, cut[1] = need - above, cut[2] = a;
+        if (above + a < need && need <= above + a + b) cut[0] = lo, cut[1] = need - above - a, cut[2] = b;
         __syncthreads();
         thr |= unsigned(cut[0]) << shift;
         mask |= unsigned(n - 1) << shift;
         need = cut[1];
         __syncthreads();
     }
-    int eq = 0;
-    each([&](int, bool in, unsigned k) { eq += __popcll(__ballot(in && k == thr)); });
-    if (lane == 0) wave_a[w] = eq;
-    __syncthreads();
+    // of the slots of that key all stay, as scores that all differ have it, or those that the waves before have are counted
     int eq0 = 0;
-    for (int i = 0; i < w; ++i) eq0 += wave_a[i];
-    __syncthreads();
+    if (uniform(cut[2]) != need) {
+        int eq = 0;
+        each([&](int, bool in, unsigned k) { eq += __popcll(__ballot(in && k == thr)); });
+        if (lane == 0) wave_a[w] = eq;
+        __syncthreads();
+        for (int i = 0; i < w; ++i) eq0 += wave_a[i];
+        __syncthreads();
+    }
     // how many holes and how many that come the waves before have; then they are written
     const unsigned long long lt = (1ull << lane) - 1;
     int* const src = p.src + (size_t(r) * p.pool.kv_heads + hk) * p.cap;
