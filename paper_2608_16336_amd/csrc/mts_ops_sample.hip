@@ -561,6 +561,14 @@ __global__ __launch_bounds__(64 * kWaves, 4) void k_sample(const SampleP p)
     if (min_w > 0.f) least = fmaxf(least, wt.top + (__logf(min_w) - 0.01f) * t * 1.0001f - 1e-30f);
     const auto sum_kept = [&](int from, int to) {
         u64 sum = 0;
+        if (!cuts && !(min_w > 0.f)) {
+            s.each(from, to, [&](int, const float x[N]) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) sum += wt.biased(wt.weight(x[e]));
+                sum -= u64(N) * wt.magic_bits;
+            });
+            return sum;
+        }
         s.each(from, to, [&](int f, const float x[N]) {
             if (fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) < least) return;
 #pragma unroll
