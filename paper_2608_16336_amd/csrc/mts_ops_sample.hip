@@ -259,6 +259,7 @@ struct Sampler {
     {
         sure = 0;
         listed = true;
+        const bool bounded = within.key != 0;  // by a rule before this one
         __syncthreads();
         if (threadIdx.x == 0) sh.above = 0;
         __syncthreads();
@@ -275,25 +276,25 @@ struct Sampler {
             __syncthreads();
             unsigned least = 0xffffffffu, most = 0;
             each([&](int f, const float x[N]) {
-                unsigned some = 0, over = 0;
+                float d[N];
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    const float d = bins_down(x[e]);
-                    over |= unsigned(d < bin) << e;
-                    some |= unsigned(d >= bin && d < next) << e;
-                }
-                if (listed && over) {
+                for (int e = 0; e < N; ++e) d[e] = bins_down(x[e]);
+                if (listed && fminf(fminf(d[0], d[1]), fminf(d[2], d[3])) < bin) {
 #pragma unroll
                     for (int e = 0; e < N; ++e) {
                         const float w = wt.weight(x[e]);
-                        const bool counts = ((over >> e) & 1) && w >= min_w && in(within, f + e, logit_key(x[e]));
+                        bool counts = d[e] < bin && w >= min_w;
+                        if (bounded) counts = counts && in(within, f + e, logit_key(x[e]));
                         sure += wt.fixed(counts ? w : 0.f);
                     }
                 }
+                bool some = false;
+#pragma unroll
+                for (int e = 0; e < N; ++e) some |= d[e] >= bin && d[e] < next;
                 if (!some) return;
 #pragma unroll
                 for (int e = 0; e < N; ++e) {
-                    if (!((some >> e) & 1) || unsigned(f + e) >= unsigned(row.vocab)) continue;
+                    if (!(d[e] >= bin && d[e] < next) || unsigned(f + e) >= unsigned(row.vocab)) continue;
                     const unsigned k = logit_key(x[e]);
                     if (!left(f + e, x[e], k)) continue;
                     least = min(least, k);
@@ -447,7 +448,7 @@ struct Sampler {
 // instructions of two exponentials a logit, and for a single row the steps
 // between the passes.  What all lanes have alike is kept in scalar registers:
 // with vector registers spilled to memory and twice the code 512 rows of
-// 100003 logits took 230 us, one row of 32768 54 us; now 137 and 37 us (rules
+// 100003 logits took 230 us, one row of 32768 54 us; now 133 and 37 us (rules
 // mixed, and top-p).
 template <class E, int kWaves>
 __global__ __launch_bounds__(64 * kWaves, 4) void k_sample(const SampleP p)
@@ -670,7 +671,7 @@ template <class E>
 static void launch_sample(const SampleP& p, uint32_t rows, hipStream_t stream)
 {
     // With a row or less a compute unit, 16 waves take one; else 8, so that two rows' passes and steps between them overlap
-    // (512 rows: 137 us with 8 waves, 163 us with 16).
+    // (512 rows took 137 us with 8 waves, 163 us with 16).
     if (rows <= 256)
         hipLaunchKernelGGL((k_sample<E, 16>), dim3(rows), dim3(1024), 0, stream, p);
     else
