@@ -678,13 +678,13 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 1 : 2) void k_attend_tiles(cons
 
 // Rows of a job and the kernel they go to.  Up to 16 rows are a stream over
 // the keys.  More take shared tiles, with four waves where that holds a
-// request's rows in one or two jobs (trees of up to 48 tokens and 5 heads: 265
-// us with 4 waves, 299 us with 8), else with eight, which read the keys half as
-// often (chunks of 2048 tokens and 4 heads: 767 us with 8, 857 us with 4).
+// request's rows in one or two jobs (trees of up to 48 tokens and 5 heads took
+// 265 us with 4 waves, 299 us with 8), else with eight, which read the keys half as
+// often (chunks of 2048 tokens and 4 heads took 767 us with 8, 857 us with 4).
 // Rows of 256 elements leave room for four waves only.
 //
 // Jobs to aim for: two a compute unit for the stream (a decode of 150 requests
-// takes 122, 100, 105, 111 us at 256, 512, 1024, 2048), fewer for the tiles,
+// takes 98, 101, 104 us at 512, 768, 1024), fewer for the tiles,
 // whose parts are large (the trees 225, 220, 238 us at 256, 384, 512).
 struct Sizes {
     uint32_t rows;    // query rows of a job

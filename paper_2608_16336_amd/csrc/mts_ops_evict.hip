@@ -23,7 +23,7 @@ constexpr int kWeighRound = 128;  // keys of one round of a workgroup: 4 waves x
 // over the query rows, 32 at a time, which lie in LDS.  Where a request has
 // more than the ROWS that fit, the job passes over its keys again for the next
 // ROWS, whose weights add to what the first pass stored (staged anew for every
-// 128 keys instead, windows of 64 tokens and 4 heads took 67 us, now 44 us).  A lane's scores S^T = K Q^T are
+// 128 keys instead, windows of 64 tokens and 4 heads took 67 us, now 43 us).  A lane's scores S^T = K Q^T are
 // 16 keys of one query: weights add up in the lane, and over the 32 lanes at
 // the end, where each step of the exchange halves what a lane still holds.
 template <class T, int D>
@@ -399,8 +399,8 @@ __global__ __launch_bounds__(256) void k_evict_move(const EvictP p, const int pi
 }
 
 // Jobs to aim for, three a compute unit as the chip holds (a decode step's
-// weights of 150 requests take 62, 63, 66, 65, 67 us at 512, 768, 1024, 1536,
-// 2048; those of six windows of 64 tokens 84, 69, 98, 71, 72 us).
+// weights of 150 requests take 60, 61, 61 us at 768, 1024, 1536; those of six
+// windows of 64 tokens 43, 61, 49 us).
 constexpr uint32_t kWeighTarget = 768;
 
 struct EvictSizes {
